@@ -19,7 +19,9 @@
  * quantize-and-pack of every window block that fills) and xq_decode_attention
  * (one query per head against the packed cache plus the window);
  * xq_decode_step runs both for every layer of a model, xq_attention_chunk
- * takes several query tokens.
+ * takes several query tokens.  xq_prefix_attention is for sequences that share a
+ * prompt, xq_cross_attention for queries that are not tokens of the cache, and
+ * xq_gather_sequences copies, forks and reorders sequences.
  *
  * Conventions that hold for every entry point:
  *   - "device" pointers are CUDA device addresses valid on the device that was
@@ -59,7 +61,7 @@ extern "C" {
 #define XQ_ERR_ORDER (-4)    /* a code-borrowing layer is ahead of the layer owning codes */
 #define XQ_ERR_CUDA (-5)     /* a CUDA call failed; xq_last_cuda_error gives the code     */
 #define XQ_ERR_NOMEM (-6)    /* host allocation failed                                    */
-#define XQ_ERR_DEVICE (-7)   /* a kernel gave up a bounded wait (xq_check_device)         */
+#define XQ_ERR_DEVICE (-7)   /* a kernel gave up a bounded wait or met a bad index (xq_check_device) */
 
 #define XQ_BF16 0 /* bfloat16 */
 #define XQ_F16 1  /* IEEE half precision */
@@ -203,6 +205,54 @@ int xq_decode_attention_f32(xq_cache* c, int layer, const void* q, float* out, v
 int xq_attention_chunk(xq_cache* c, int layer, const void* q, void* out, int n_q_tokens, void* stream);
 int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, int n_q_tokens, void* stream);
 
+/* Attention of a batch whose sequences share a prompt: `prefix` holds the prompt once, `c` what follows
+ * it in each sequence.  Sequence b of c continues sequence b / (batch of c / batch of prefix) of prefix, whose
+ * batch divides c's (1: one prompt for all; several prompts with as many samples each).  Query token j
+ * (0 .. n_q_tokens - 1) of a sequence attends to all tokens of its prefix, then to its own tokens
+ * 0 .. S - n_q_tokens + j as xq_attention_chunk has it (S the layer's length in c; S = 0: the prefix alone;
+ * else n_q_tokens <= S), under one softmax.  q, out: device, [n_q_tokens, batch of c, n_q_heads, head_dim]
+ * contiguous, io_dtype, 16-byte aligned; one token is a decode call.  The prefix is read once for every 128
+ * query rows (tokens x sequences x heads of a kv head), and nothing of it is written: several caches may use it
+ * at once, ordered after the calls that filled it.  The handles agree in n_layers, heads, head_dim, io_dtype
+ * and softmax scale; bits, groups, windows and sharing may differ (else XQ_ERR_CONFIG; also c = prefix).
+ * workspace: device, 16-byte aligned, at least xq_prefix_workspace_bytes(c, prefix, n_q_tokens) bytes (which
+ * no length changes), contents arbitrary; calls that may overlap on the GPU need one each, and calls through
+ * one handle c are ordered by the caller, as all calls of a handle are.  A call captured into a graph keeps the
+ * lengths it was captured with.
+ * Precision: codes, scales and zero-points enter the matrix products exactly, q as half precision relative to
+ * the row's largest element, the softmax numerators are rounded to half precision (2^-12 of each; their sum is
+ * that of the rounded ones), sums are fp32.  XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.
+ * The _f32 variant writes float results (tests).  Errors as xq_attention_chunk; XQ_ERR_ARG also: both layers
+ * empty, 0 < S < n_q_tokens, current device not the handles'; XQ_ERR_CAPACITY: workspace too small. */
+size_t xq_prefix_workspace_bytes(const xq_cache* c, const xq_cache* prefix, int n_q_tokens);
+int xq_prefix_attention(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* out, int n_q_tokens,
+                        void* workspace, size_t workspace_bytes, void* stream);
+int xq_prefix_attention_f32(xq_cache* c, xq_cache* prefix, int layer, const void* q, float* out, int n_q_tokens,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Cross attention: n_q_tokens >= 1 query tokens of each sequence (any number: they are not tokens of the cache)
+ * against all tokens of `layer` (an encoder's states, say), none masked.  lengths: device, int32 [batch], or
+ * NULL; sequence b has only its first lengths[b] tokens (values outside 0 .. S count as the nearer end), and
+ * what the cache holds behind them reaches no result.  Length 0 gives zeros.  q, out, workspace, precision as
+ * xq_prefix_attention.  Errors: XQ_ERR_ARG (also: empty layer), XQ_ERR_ORDER, XQ_ERR_CAPACITY, XQ_ERR_CUDA. */
+size_t xq_cross_workspace_bytes(const xq_cache* c, int n_q_tokens);
+int xq_cross_attention(xq_cache* c, int layer, const void* q, void* out, int n_q_tokens, const int32_t* lengths,
+                       void* workspace, size_t workspace_bytes, void* stream);
+int xq_cross_attention_f32(xq_cache* c, int layer, const void* q, float* out, int n_q_tokens, const int32_t* lengths,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies sequences: sequence b of `dst` becomes sequence index[b] of `src`, in every layer, with codes, scales,
+ * zero-points and window, and dst takes src's lengths.  index: device, int32 [batch of dst]; a source may be
+ * named several times or not at all.  A prompt is forked (batch 1 to n), finished sequences are left out (n to
+ * fewer), the beams of a search reordered: dst = src does that in place, for any index (at most 1505 sequences;
+ * more: XQ_ERR_CAPACITY).  The handles agree in everything that gives the bytes a meaning (n_layers, n_kv_heads,
+ * head_dim, group_size, residual_len, kq, vq, km, vm, io_dtype, sharing pattern, gamma1), else XQ_ERR_CONFIG;
+ * batch, max_seq, query heads, kernel and calibration may differ.  An index outside 0 .. batch of src - 1 leaves
+ * its sequence's bytes as they are and is reported by xq_check_device(dst) as XQ_ERR_DEVICE.  The code
+ * difference counters are not copied.  One launch for up to 32 layers; the lengths change at once on the host.
+ * Errors: XQ_ERR_ARG, XQ_ERR_CONFIG, XQ_ERR_CAPACITY (a layer longer than dst's max_seq), XQ_ERR_CUDA. */
+int xq_gather_sequences(xq_cache* dst, const xq_cache* src, const int32_t* index, void* stream);
+
 /* xq_decode_attention for callers that cannot provide scratch memory of their
  * own.  (The paper has no counterpart: this is a deployment variant, not part of
  * the method.)  Some hosts hand every byte of device memory to their own pools at
@@ -265,7 +315,7 @@ int xq_decode_step(xq_cache* c, const void* K_new, const void* V_new, const void
                    const int32_t* layer_order, int mem, void* stream);
 
 /* Waits for `stream` and reports whether a kernel launched through this handle
- * gave up one of its bounded waits (XQ_ERR_DEVICE; the outputs of that call are
+ * gave up one of its bounded waits or met an index out of range (XQ_ERR_DEVICE; the outputs of that call are
  * then invalid and the handle should be reset) -- every wait inside the kernels
  * has an iteration limit instead of the ability to hang the GPU.  XQ_OK otherwise.
  * Synchronizes; not for the hot path. */

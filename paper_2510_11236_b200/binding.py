@@ -54,6 +54,17 @@ _SIGNATURES = {
                                           ctypes.c_void_p]),
     "xq_attention_chunk_f32": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
                                               ctypes.c_int, ctypes.c_void_p]),
+    "xq_prefix_workspace_bytes": (ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int]),
+    "xq_prefix_attention": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "xq_prefix_attention_f32": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                               ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "xq_cross_workspace_bytes": (ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_int]),
+    "xq_cross_attention": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "xq_cross_attention_f32": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "xq_gather_sequences": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "xq_decode_step": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                       ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32), ctypes.c_int,
                                       ctypes.c_void_p]),
@@ -159,6 +170,35 @@ def xq_attention_chunk(handle, layer: int, q, out, n_q_tokens: int, stream: int 
 
 def xq_attention_chunk_f32(handle, layer: int, q, out, n_q_tokens: int, stream: int = 0) -> int:
     return lib().xq_attention_chunk_f32(handle, layer, _ptr(q), _ptr(out), n_q_tokens, stream)
+
+
+def xq_prefix_workspace_bytes(handle, prefix, n_q_tokens: int) -> int:
+    return lib().xq_prefix_workspace_bytes(handle, prefix, n_q_tokens)
+
+
+def xq_prefix_attention(handle, prefix, layer: int, q, out, n_q_tokens: int, workspace, nbytes: int, stream: int = 0) -> int:
+    return lib().xq_prefix_attention(handle, prefix, layer, _ptr(q), _ptr(out), n_q_tokens, _ptr(workspace), nbytes, stream)
+
+
+def xq_prefix_attention_f32(handle, prefix, layer: int, q, out, n_q_tokens: int, workspace, nbytes: int, stream: int = 0) -> int:
+    return lib().xq_prefix_attention_f32(handle, prefix, layer, _ptr(q), _ptr(out), n_q_tokens, _ptr(workspace), nbytes, stream)
+
+
+def xq_cross_workspace_bytes(handle, n_q_tokens: int) -> int:
+    return lib().xq_cross_workspace_bytes(handle, n_q_tokens)
+
+
+def xq_cross_attention(handle, layer: int, q, out, n_q_tokens: int, lengths, workspace, nbytes: int, stream: int = 0) -> int:
+    return lib().xq_cross_attention(handle, layer, _ptr(q), _ptr(out), n_q_tokens, _ptr(lengths), _ptr(workspace), nbytes, stream)
+
+
+def xq_cross_attention_f32(handle, layer: int, q, out, n_q_tokens: int, lengths, workspace, nbytes: int, stream: int = 0) -> int:
+    return lib().xq_cross_attention_f32(handle, layer, _ptr(q), _ptr(out), n_q_tokens, _ptr(lengths), _ptr(workspace), nbytes,
+                                        stream)
+
+
+def xq_gather_sequences(handle, src, index, stream: int = 0) -> int:
+    return lib().xq_gather_sequences(handle, src, _ptr(index), stream)
 
 
 def xq_decode_step(handle, K_new, V_new, q, out, layer_order=None, mem: int = XQ_MEM_DEVICE, stream: int = 0) -> int:
@@ -304,6 +344,53 @@ class Cache:
         if rc:
             raise XQError(rc, "xq_attention_chunk")
         return out
+
+    def _rows_call(self, name, q, out, f32, workspace, need, call):
+        """Checks the tensors of a prefix or cross attention call, makes what was not given, and makes the call."""
+        import torch
+        if (q.dim() != 4 or tuple(q.shape[1:]) != (self.cfg.batch, self.cfg.n_q_heads, self.cfg.head_dim)
+                or q.dtype != (torch.float16 if self.cfg.io_dtype == XQ_F16 else torch.bfloat16)):
+            raise ValueError(f"{name}: q is [n_q_tokens, batch, n_q_heads, head_dim] of the cache's io_dtype")
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.float32 if f32 else q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != (torch.float32 if f32 else q.dtype):
+            raise ValueError(f"{name}: out has q's shape, and q's type or float32 with f32")
+        if workspace is None:
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=self.workspace.device)
+        if any(t.device != self.workspace.device for t in (q, out, workspace)):
+            raise ValueError(f"{name}: tensors on the cache's device")
+        rc = call(q, out, q.shape[0], workspace, workspace.numel() * workspace.element_size())
+        if rc:
+            raise XQError(rc, name)
+        return out
+
+    def prefix_attention(self, prefix, layer, q, out=None, f32=False, workspace=None):
+        """q: [n_q_tokens, batch, n_q_heads, head_dim]; prefix: the Cache that every batch / prefix batch sequences share.
+        workspace: xq_prefix_workspace_bytes bytes, made here if not given."""
+        fn = xq_prefix_attention_f32 if f32 else xq_prefix_attention
+        need = xq_prefix_workspace_bytes(self.handle, prefix.handle, q.shape[0]) if workspace is None else 0
+        return self._rows_call("xq_prefix_attention", q, out, f32, workspace, need, lambda q, out, n, w, size: fn(
+            self.handle, prefix.handle, layer, q, out, n, w, size, self._stream()))
+
+    def cross_attention(self, layer, q, lengths=None, out=None, f32=False, workspace=None):
+        """q: [n_q_tokens, batch, n_q_heads, head_dim]; lengths: int32 [batch] on the device, or None: all tokens."""
+        import torch
+        if lengths is not None and (lengths.dtype != torch.int32 or tuple(lengths.shape) != (self.cfg.batch,)
+                                    or lengths.device != self.workspace.device):
+            raise ValueError("xq_cross_attention: lengths is int32 [batch] on the cache's device")
+        fn = xq_cross_attention_f32 if f32 else xq_cross_attention
+        need = xq_cross_workspace_bytes(self.handle, q.shape[0]) if workspace is None else 0
+        return self._rows_call("xq_cross_attention", q, out, f32, workspace, need, lambda q, out, n, w, size: fn(
+            self.handle, layer, q, out, n, lengths, w, size, self._stream()))
+
+    def gather_sequences(self, src, index):
+        """Sequence b becomes sequence index[b] of the Cache `src` (this one: in place).  index: int32 [batch] on the device."""
+        import torch
+        if index.dtype != torch.int32 or tuple(index.shape) != (self.cfg.batch,) or index.device != self.workspace.device:
+            raise ValueError("xq_gather_sequences: index is int32 [batch] on the cache's device")
+        rc = xq_gather_sequences(self.handle, src.handle, index, self._stream())
+        if rc:
+            raise XQError(rc, "xq_gather_sequences")
 
     def decode_step(self, K_new, V_new, q, out, layer_order=None, mem=XQ_MEM_DEVICE):
         rc = xq_decode_step(self.handle, K_new, V_new, q, out, layer_order, mem, self._stream())

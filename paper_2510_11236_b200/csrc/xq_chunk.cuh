@@ -817,6 +817,7 @@ __global__ void __launch_bounds__(C_THREADS, 1) chunk_kernel(const __grid_consta
       }
       if (p.ns > 1 && w == 0 && r < n_rows)
         *reinterpret_cast<float2*>(p.part_ml + ((part0 + r) * p.ns + split) * 2) = make_float2(M, L);
+      if (p.ns == 1 && w == 0 && r < n_rows && p.lse != nullptr) p.lse[out_row(r)] = M + log2f(L) - (float)C_PEXP;
     }
   }
   tc_fence_before();
@@ -855,6 +856,7 @@ __global__ void __launch_bounds__(C_THREADS, 1) chunk_kernel(const __grid_consta
       Ls = fmaf(x.y, f, Ls);
     }
     const float inv = 1.0f / Ls;
+    if (d == 0 && p.lse != nullptr) p.lse[out_row(r)] = Mx + log2f(Ls) - (float)C_PEXP;
     chunk_store<D>(p, out_row(r), d, ax * inv);
     chunk_store<D>(p, out_row(r), d + 1, ay * inv);
   }

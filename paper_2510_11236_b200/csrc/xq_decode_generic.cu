@@ -172,6 +172,7 @@ __global__ void merge_kernel(MergeParams p) {
     A += p.part_acc[(base + s) * D + d] * f;
   }
   float o = A / Lsum;
+  if (d == 0 && p.lse != nullptr) p.lse[(size_t)b * dm.Hq + hq] = M + log2f(Lsum);
   size_t oi = ((size_t)b * dm.Hq + hq) * D + d;
   if (p.out_f32)
     reinterpret_cast<float*>(p.out)[oi] = o;

@@ -316,7 +316,10 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
-    if (lane == 0) w[ns] = 1.0f / Ls;
+    if (lane == 0) {
+      w[ns] = 1.0f / Ls;
+      if (NL == 1 && p.lse != nullptr) p.lse[row_of(v)] = M + log2f(Ls);
+    }
   }
   __syncthreads();
   for (int item = threadIdx.x; item < NL * dm.G * (D / 4); item += blockDim.x) {
@@ -1308,6 +1311,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
       store_out(p, LL[layer], hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
+      if (NL == 1 && d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
     } else {
       const size_t at = ((size_t)layer * dm.B * dm.Hq + hq) * p.ns_q + split;
       *reinterpret_cast<float4*>(part_acc + at * D + d) = A;

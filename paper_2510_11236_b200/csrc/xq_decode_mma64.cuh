@@ -268,7 +268,10 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
-    if (lane == 0) w[ns] = 1.0f / Ls;
+    if (lane == 0) {
+      w[ns] = 1.0f / Ls;
+      if (p.lse != nullptr) p.lse[hq0 + h] = M + log2f(Ls);
+    }
   }
   __syncthreads();
   for (int item = threadIdx.x; item < dm.G * (D / 4); item += blockDim.x) {
@@ -986,6 +989,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
       store_out(p, L, hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
+      if (d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
     } else {
       *reinterpret_cast<float4*>(part_acc + (hq * p.ns_q + split) * D + d) = A;
       if (d == 0) *reinterpret_cast<float2*>(part_ml + (hq * p.ns_q + split) * 2) = make_float2(M, Ls);

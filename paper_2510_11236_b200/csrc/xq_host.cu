@@ -120,6 +120,11 @@ void make_plan(const xq_config* c, Plan& pl) {
   pl.total = off;
 }
 
+// Rows calls (prefix and cross attention): CTAs that splits make, at most, in waves of the device; what a CTA's start and end
+// and a partial of a row cost, in tiles of 64 tokens.
+constexpr int ROWS_WAVES = 4;
+constexpr double ROWS_FIXED = 8.0, ROWS_JOIN = 1e-4;
+
 constexpr int N_KINDS = 4;
 constexpr int TIMING_POOL = 1 << 15;
 
@@ -489,6 +494,7 @@ int prepare_decode(const xq_cache* c, int layer, const void* q, void* out, int o
   p.early_fetch = 0;
   p.late_wait = 0;
   p.f16 = c->cfg.io_dtype == XQ_F16;
+  p.lse = nullptr;
   return XQ_OK;
 }
 
@@ -514,6 +520,7 @@ int launch_decode(xq_cache* c, DecodeParams& p, bool use_mma, const Scratch& s, 
   m.part_ml = p.part_ml;
   m.out = p.layer[0].out;
   m.out_f32 = p.out_f32;
+  m.lse = p.lse;
   {
     Timer t(c, st, 1);
     e = launch_merge(m, st);
@@ -622,7 +629,7 @@ int pack_layers(xq_cache* c, const int* layers, int n, const void* K, const void
 // launch reads (q, the new token, the window, the packed streams) can still be written when its CTAs start; it
 // waits for that launch only before it writes.  *was_mma tells the caller whether this launch can head such a chain.
 int decode_impl(xq_cache* c, int layer, const void* q, void* out, int out_f32, cudaStream_t st, int vis = -1,
-                bool chained = false, bool* was_mma = nullptr) {
+                bool chained = false, bool* was_mma = nullptr, float* lse = nullptr) {
   if (was_mma) *was_mma = false;
   if (!c) return XQ_ERR_ARG;
   if (layer < 0 || layer >= c->cfg.n_layers) return XQ_ERR_ARG;
@@ -630,6 +637,7 @@ int decode_impl(xq_cache* c, int layer, const void* q, void* out, int out_f32, c
   bool use_mma = false;
   int rc = prepare_decode(c, layer, q, out, out_f32, nullptr, nullptr, c->seq[layer], p, use_mma, vis);
   if (rc != XQ_OK) return rc;
+  p.lse = lse;
   if (use_mma) {
     rc = ensure_clean_scratch(c, st);
     if (rc != XQ_OK) return rc;
@@ -919,7 +927,7 @@ bool tokens_one_by_one(const xq_cache* c, int layer, int T) {
   return plan.alone + (T - 1) * plan.next < chunk;
 }
 
-int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int out_f32, cudaStream_t st) {
+int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int out_f32, float* lse, cudaStream_t st) {
   int rc = ensure_clean_scratch(c, st);
   if (rc != XQ_OK) return rc;
   const Dims& dm = c->plan.dm;
@@ -943,6 +951,7 @@ int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int ou
   p.status = s.status;
   p.out_f32 = out_f32;
   p.f16 = c->cfg.io_dtype == XQ_F16;
+  p.lse = lse;
   cudaError_t e;
   {
     Timer t(c, st, 0);
@@ -959,7 +968,7 @@ int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int ou
 
 // Query token j of n sees the cache up to its own position.  One launch of the chunk kernel, or (few tokens, the scalar
 // kernel) one decode launch per token, all on the same stream.
-int chunk_impl(xq_cache* c, int layer, const void* q, void* out, int n, int out_f32, void* stream) {
+int chunk_impl(xq_cache* c, int layer, const void* q, void* out, int n, int out_f32, void* stream, float* lse = nullptr) {
   if (!c || !q || !out) return XQ_ERR_ARG;
   if (layer < 0 || layer >= c->cfg.n_layers) return XQ_ERR_ARG;
   const int S = c->seq[layer];
@@ -974,13 +983,14 @@ int chunk_impl(xq_cache* c, int layer, const void* q, void* out, int n, int out_
     if (rc == XQ_OK) rc = check_decode(c, layer, q, out, nullptr, nullptr, S, S, nq, r, use_mma);
     if (rc != XQ_OK) return rc;
   }
-  if (use_mma && n > 1 && !tokens_one_by_one(c, layer, n)) return launch_chunk(c, layer, q, out, n, out_f32, (cudaStream_t)stream);
+  if (use_mma && n > 1 && !tokens_one_by_one(c, layer, n)) return launch_chunk(c, layer, q, out, n, out_f32, lse, (cudaStream_t)stream);
   const size_t row = (size_t)dm.B * dm.Hq * dm.D;  // elements of one token's queries: [batch, heads, head_dim]
   bool chain = false;  // launches after the first read what the first one waited for and write their own rows
   for (int j = 0; j < n; ++j) {
     const uint8_t* qj = (const uint8_t*)q + (size_t)j * row * 2;
     uint8_t* oj = (uint8_t*)out + (size_t)j * row * (out_f32 ? 4 : 2);
-    const int rc = decode_impl(c, layer, qj, oj, out_f32, (cudaStream_t)stream, S - n + 1 + j, chain, &chain);
+    const int rc = decode_impl(c, layer, qj, oj, out_f32, (cudaStream_t)stream, S - n + 1 + j, chain, &chain,
+                               lse ? lse + (size_t)j * dm.B * dm.Hq : nullptr);
     if (rc != XQ_OK) return rc;
   }
   return XQ_OK;
@@ -993,6 +1003,300 @@ int xq_attention_chunk(xq_cache* c, int layer, const void* q, void* out, int n_q
 
 int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, int n_q_tokens, void* stream) {
   return chunk_impl(c, layer, q, out, n_q_tokens, 1, stream);
+}
+
+namespace {
+
+// ---- attention over a whole cache for many query rows (prefix and cross attention) ----
+
+// Splits of the tokens that a rows call can ask for, whatever the cache's length: a workspace of that many partials serves
+// every length.
+int rows_most_splits(const xq_cache* kv, long long ctas) {
+  const long long tiles = (kv->cfg.max_seq + 127) / 128 + 1, waves = (ROWS_WAVES * (long long)kv->sm_count + ctas - 1) / ctas;
+  return (int)std::max(1LL, std::min(tiles, waves));
+}
+
+struct RowsPlan {
+  int each, row_tiles;
+  long long rows;   // of the call
+  long long ctas;   // streams x row tiles
+};
+RowsPlan rows_plan(const xq_cache* kv, int Bq, int T) {
+  const Dims& dm = kv->plan.dm;
+  RowsPlan r;
+  r.each = Bq / dm.B;
+  r.row_tiles = (int)(((long long)T * r.each * dm.G + ROWS_TILE - 1) / ROWS_TILE);
+  r.rows = (long long)T * Bq * dm.Hq;
+  r.ctas = (long long)r.row_tiles * dm.B * dm.Hkv;
+  return r;
+}
+
+// Splits of a call: modelled times in units of a 64-token tile.  A launch's CTAs go in waves; a CTA costs its tiles and
+// ROWS_FIXED more, and a partial that is written and read again costs each row something.
+int rows_splits(const xq_cache* kv, const RowsPlan& r, int S) {
+  const int batches = (S + 127) / 128, most = std::min(rows_most_splits(kv, r.ctas), std::max(1, batches));
+  int best = 1;
+  double best_time = 0.0;
+  for (int ns = 1; ns <= most; ++ns) {
+    const double waves = ceil((double)(r.ctas * ns) / kv->sm_count), tiles = 2.0 * ((batches + ns - 1) / ns);
+    const double time = waves * (tiles + ROWS_FIXED) + (ns > 1 ? ROWS_JOIN * (double)r.rows * ns : 0.0);
+    if (ns == 1 || time < best_time) {
+      best = ns;
+      best_time = time;
+    }
+  }
+  return best;
+}
+
+// Parts of a call's workspace, in bytes from its start.
+struct RowsScratch {
+  size_t part_acc, part_ml, own, own_lse, total;
+};
+RowsScratch rows_scratch(const RowsPlan& r, int ns, int D, bool own) {
+  RowsScratch s;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+  s.part_acc = take((size_t)r.rows * ns * D * 4);
+  s.part_ml = take((size_t)r.rows * ns * 8);
+  s.own = take(own ? (size_t)r.rows * D * 4 : 0);
+  s.own_lse = take(own ? (size_t)r.rows * 4 : 0);
+  s.total = off;
+  return s;
+}
+
+// Rows of a stream are counted in 32 bits, and so are the CTAs of a launch.
+bool rows_fit(const xq_cache* kv, int Bq, int T) {
+  return T >= 1 && (long long)T * (Bq / kv->cfg.batch) * kv->plan.dm.G <= (1LL << 30) && (long long)T * Bq * kv->cfg.n_q_heads <= (1LL << 31);
+}
+
+// The rows of one call over kv's layer: partials in the workspace (or the result itself, where one split has all of it).
+// status: device word of the handle that the call reports through.
+int launch_rows(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, int T, int ns, const int* lengths, const void* q,
+                void* out, int out_f32, float* part_acc, float* part_ml, cudaStream_t st) {
+  const Dims& dm = kv->plan.dm;
+  const int S = kv->seq[layer];
+  RowsParams p;
+  p.dm = dm;
+  p.L = layer_ptrs(kv, layer);
+  p.q = (const uint16_t*)q;
+  p.r = residual_count(S, dm.R);
+  p.n_q = S - p.r;
+  p.lengths = lengths;
+  p.T = T;
+  p.each = r.each;
+  p.row_tiles = r.row_tiles;
+  p.ns = ns;
+  p.scale = c->scale;
+  p.part_acc = part_acc;
+  p.part_ml = part_ml;
+  p.out = out;
+  p.out_f32 = out_f32;
+  p.f16 = kv->cfg.io_dtype == XQ_F16;
+  p.status = workspace_scratch(c).status;
+  cudaError_t e;
+  {
+    Timer t(c, st, 0);
+    e = launch_rows_generic(p, st);
+  }
+  c->launches++;
+  return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
+}
+
+int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_acc, const float* part_ml, const float* own,
+                     const float* own_lse, void* out, int out_f32, cudaStream_t st) {
+  JoinParams p;
+  p.rows = r.rows;
+  p.D = c->cfg.head_dim;
+  p.ns = ns;
+  p.part_acc = part_acc;
+  p.part_ml = part_ml;
+  p.own = own;
+  p.own_lse = own_lse;
+  p.out = out;
+  p.out_f32 = out_f32;
+  p.f16 = c->cfg.io_dtype == XQ_F16;
+  cudaError_t e;
+  {
+    Timer t(c, st, 1);
+    e = launch_join(p, st);
+  }
+  c->launches++;
+  return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
+}
+
+// Whether the handle's device is the current one (a handle made without a device has none).
+bool on_device(const xq_cache* c) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) cudaGetLastError();
+  return dev == c->device;
+}
+
+// Whether sequences of `c` can attend to the caches of `prefix`.
+bool prefix_fits(const xq_cache* c, const xq_cache* prefix) {
+  const xq_config &a = c->cfg, &b = prefix->cfg;
+  return c != prefix && a.n_layers == b.n_layers && a.n_q_heads == b.n_q_heads && a.n_kv_heads == b.n_kv_heads &&
+         a.head_dim == b.head_dim && a.io_dtype == b.io_dtype && c->scale == prefix->scale && a.batch % b.batch == 0;
+}
+
+int prefix_impl(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* out, int T, int out_f32, void* workspace,
+                size_t bytes, void* stream) {
+  if (!c || !prefix || !q || !out) return XQ_ERR_ARG;
+  if (!prefix_fits(c, prefix)) return XQ_ERR_CONFIG;
+  if (layer < 0 || layer >= c->cfg.n_layers || !rows_fit(prefix, c->cfg.batch, T)) return XQ_ERR_ARG;
+  if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return XQ_ERR_ARG;
+  const int S = c->seq[layer], Sp = prefix->seq[layer];
+  if (S + Sp == 0 || (S > 0 && S < T)) return XQ_ERR_ARG;
+  if (Sp == 0) return chunk_impl(c, layer, q, out, T, out_f32, stream);
+  int nq, r;
+  bool use_mma;
+  int rc = check_decode(prefix, layer, q, out, nullptr, nullptr, Sp, -1, nq, r, use_mma);
+  if (rc == XQ_OK && S > 0) rc = check_decode(c, layer, q, out, nullptr, nullptr, S, S - T + 1, nq, r, use_mma);
+  if (rc == XQ_OK && S > 0) rc = check_decode(c, layer, q, out, nullptr, nullptr, S, S, nq, r, use_mma);
+  if (rc != XQ_OK) return rc;
+  const RowsPlan plan = rows_plan(prefix, c->cfg.batch, T);
+  const int ns = rows_splits(prefix, plan, Sp);
+  const RowsScratch s = rows_scratch(plan, ns, c->cfg.head_dim, S > 0);
+  if (!workspace || ((uintptr_t)workspace & 15)) return XQ_ERR_ARG;
+  if (bytes < s.total) return XQ_ERR_CAPACITY;
+  if (!on_device(c) || prefix->device != c->device) return XQ_ERR_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  rc = ensure_clean_scratch(c, st);
+  if (rc != XQ_OK) return rc;
+  uint8_t* w = (uint8_t*)workspace;
+  float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml), *own = nullptr, *lse = nullptr;
+  if (S > 0) {
+    own = (float*)(w + s.own);
+    lse = (float*)(w + s.own_lse);
+    rc = chunk_impl(c, layer, q, own, T, 1, stream, lse);
+    if (rc != XQ_OK) return rc;
+  }
+  rc = launch_rows(c, prefix, layer, plan, T, ns, nullptr, q, out, out_f32, acc, ml, st);
+  if (rc != XQ_OK) return rc;
+  return launch_rows_join(c, plan, ns, acc, ml, own, lse, out, out_f32, st);
+}
+
+int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const int32_t* lengths, int out_f32, void* workspace,
+               size_t bytes, void* stream) {
+  if (!c || !q || !out) return XQ_ERR_ARG;
+  if (layer < 0 || layer >= c->cfg.n_layers || !rows_fit(c, c->cfg.batch, T)) return XQ_ERR_ARG;
+  if (((uintptr_t)q & 15) || ((uintptr_t)out & 15) || ((uintptr_t)lengths & 3)) return XQ_ERR_ARG;
+  const int S = c->seq[layer];
+  int nq, r;
+  bool use_mma;
+  int rc = check_decode(c, layer, q, out, nullptr, nullptr, S, -1, nq, r, use_mma);
+  if (rc != XQ_OK) return rc;
+  const RowsPlan plan = rows_plan(c, c->cfg.batch, T);
+  const int ns = rows_splits(c, plan, S);
+  const RowsScratch s = rows_scratch(plan, ns, c->cfg.head_dim, false);
+  if (!workspace || ((uintptr_t)workspace & 15)) return XQ_ERR_ARG;
+  if (bytes < s.total) return XQ_ERR_CAPACITY;
+  if (!on_device(c)) return XQ_ERR_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  rc = ensure_clean_scratch(c, st);
+  if (rc != XQ_OK) return rc;
+  uint8_t* w = (uint8_t*)workspace;
+  float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml);
+  rc = launch_rows(c, c, layer, plan, T, ns, lengths, q, out, out_f32, acc, ml, st);
+  if (rc != XQ_OK) return rc;
+  return launch_rows_join(c, plan, ns, acc, ml, nullptr, nullptr, out, out_f32, st);
+}
+
+// Whether a cache of `src`'s data can be held by `dst`: everything that decides what the bytes of a sequence mean.
+bool same_contents(const xq_config& a, const xq_config& b) {
+  return a.n_layers == b.n_layers && a.n_kv_heads == b.n_kv_heads && a.head_dim == b.head_dim && a.group_size == b.group_size &&
+         a.residual_len == b.residual_len && a.kq == b.kq && a.vq == b.vq && a.km == b.km && a.vm == b.vm &&
+         a.io_dtype == b.io_dtype && share_group_of(&a) == share_group_of(&b) && a.share_dominant == b.share_dominant &&
+         a.gamma1 == b.gamma1;
+}
+
+}  // namespace
+
+size_t xq_prefix_workspace_bytes(const xq_cache* c, const xq_cache* prefix, int n_q_tokens) {
+  if (!c || !prefix || !prefix_fits(c, prefix) || !rows_fit(prefix, c->cfg.batch, n_q_tokens)) return 0;
+  const RowsPlan r = rows_plan(prefix, c->cfg.batch, n_q_tokens);
+  return rows_scratch(r, rows_most_splits(prefix, r.ctas), c->cfg.head_dim, true).total;
+}
+
+size_t xq_cross_workspace_bytes(const xq_cache* c, int n_q_tokens) {
+  if (!c || !rows_fit(c, c->cfg.batch, n_q_tokens)) return 0;
+  const RowsPlan r = rows_plan(c, c->cfg.batch, n_q_tokens);
+  return rows_scratch(r, rows_most_splits(c, r.ctas), c->cfg.head_dim, false).total;
+}
+
+int xq_prefix_attention(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* out, int n_q_tokens, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  return prefix_impl(c, prefix, layer, q, out, n_q_tokens, 0, workspace, workspace_bytes, stream);
+}
+
+int xq_prefix_attention_f32(xq_cache* c, xq_cache* prefix, int layer, const void* q, float* out, int n_q_tokens, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  return prefix_impl(c, prefix, layer, q, out, n_q_tokens, 1, workspace, workspace_bytes, stream);
+}
+
+int xq_cross_attention(xq_cache* c, int layer, const void* q, void* out, int n_q_tokens, const int32_t* lengths, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  return cross_impl(c, layer, q, out, n_q_tokens, lengths, 0, workspace, workspace_bytes, stream);
+}
+
+int xq_cross_attention_f32(xq_cache* c, int layer, const void* q, float* out, int n_q_tokens, const int32_t* lengths,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  return cross_impl(c, layer, q, out, n_q_tokens, lengths, 1, workspace, workspace_bytes, stream);
+}
+
+int xq_gather_sequences(xq_cache* dst, const xq_cache* src, const int32_t* index, void* stream) {
+  if (!dst || !src || !index || ((uintptr_t)index & 3)) return XQ_ERR_ARG;
+  if (!same_contents(dst->cfg, src->cfg)) return XQ_ERR_CONFIG;
+  const int L = src->cfg.n_layers;
+  for (int l = 0; l < L; ++l)
+    if (src->seq[l] > dst->cfg.max_seq) return XQ_ERR_CAPACITY;
+  if (dst == src && dst->cfg.batch > gather_place_limit()) return XQ_ERR_CAPACITY;
+  if (!on_device(dst) || src->device != dst->device) return XQ_ERR_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  const int rc = ensure_clean_scratch(dst, st);
+  if (rc != XQ_OK) return rc;
+  const Dims &ds = src->plan.dm, &dd = dst->plan.dm;
+  GatherParams p;
+  p.src = src->ws;
+  p.dst = dst->ws;
+  p.index = index;
+  p.B_src = ds.B;
+  p.B_dst = dd.B;
+  p.Hkv = ds.Hkv;
+  p.D = ds.D;
+  p.g = ds.g;
+  p.NG = ds.NG;
+  p.R = ds.R;
+  p.src_cap = ds.nq_cap;
+  p.dst_cap = dd.nq_cap;
+  p.status = workspace_scratch(dst).status;
+  for (int l0 = 0; l0 < L; l0 += GATHER_MAX_LAYERS) {
+    p.n_layers = std::min(GATHER_MAX_LAYERS, L - l0);
+    for (int i = 0; i < p.n_layers; ++i) {
+      const int l = l0 + i;
+      GatherLayer& g = p.layer[i];
+      const LayerRegions &a = src->plan.layers[l], &b = dst->plan.layers[l];
+      const size_t from[6] = {a.k_codes, a.v_codes, a.k_meta, a.v_meta, a.win_k, a.win_v};
+      const size_t to[6] = {b.k_codes, b.v_codes, b.k_meta, b.v_meta, b.win_k, b.win_v};
+      for (int w = 0; w < 6; ++w) {
+        g.src[w] = (uint32_t)(from[w] / 256);
+        g.dst[w] = (uint32_t)(to[w] / 256);
+      }
+      g.r = residual_count(src->seq[l], ds.R);
+      g.n_q = src->seq[l] - g.r;
+      g.bk = k_owner(&src->cfg, l) == l ? layer_bits(l, src->cfg.kq) : 0;
+      g.bv = v_owner(&src->cfg, l) == l ? layer_bits(l, src->cfg.vq) : 0;
+    }
+    cudaError_t e;
+    {
+      Timer t(dst, st, 3);
+      e = launch_gather(p, st);
+    }
+    dst->launches++;
+    if (e != cudaSuccess) return fail_cuda(dst, e);
+  }
+  for (int l = 0; l < L; ++l) dst->seq[l] = src->seq[l];
+  for (auto& x : dst->repacked) x = 1;  // the next decode of every layer waits for this launch
+  return XQ_OK;
 }
 
 int xq_decode_attention_static(xq_cache* c, int layer, const void* q, void* out, void* stream) {

@@ -112,6 +112,9 @@ struct DecodeParams {
   int late_wait;
   int* status;  // device word the tensor-core kernel sets when one of its bounded waits gave up
   int f16;      // q, the window and the 16-bit output are IEEE half precision (else bfloat16)
+  // [B,Hq] or null (launches of one layer): log2 of each result's softmax denominator, sum 2^(logit / ln 2), for callers
+  // that join the result with another one over other tokens
+  float* lse;
   DecodeLayer layer[DECODE_MAX_LAYERS];
 };
 
@@ -133,6 +136,7 @@ struct ChunkParams {
   unsigned int* tickets;  // [row_tiles,B*Hkv], zero between launches
   int* status;        // device word that is set when a bounded wait gave up
   int out_f32, f16;
+  float* lse;         // [T,B,Hq] or null: as in DecodeParams
 };
 
 struct MergeParams {
@@ -143,6 +147,62 @@ struct MergeParams {
   const float* part_ml;
   void* out;
   int out_f32;
+  float* lse;  // [B,Hq] or null: as in DecodeParams
+};
+
+// Attention of query rows over all tokens of a cache, none masked but for the sequences' lengths (xq_rows.cuh).  Sequence u
+// of the cache serves the sequences u * each .. u * each + each - 1 of the queries.  A row is (token j, one of these
+// sequences i, head h of a kv head): row (j * each + i) * G + h of its stream, and row (j * Bq + u * each + i) * Hq + hk * G
+// + h of the call.
+struct RowsParams {
+  Dims dm;             // of the cache (B: its sequences)
+  LayerPtrs L;
+  const uint16_t* q;   // [T,Bq,Hq,D], Bq = B * each
+  int n_q, r;          // tokens of the cache: packed, window
+  const int* lengths;  // [B] or null: the tokens of each sequence that exist
+  int T, each;
+  int row_tiles;       // per (sequence, kv head): T * each * G rows over ROWS_TILE
+  int ns;              // splits of the tokens
+  float scale;
+  // null: the result goes to out, else [rows of the call,ns,D] sums of numerators times values and [rows,ns,2] (reference
+  // in log2 units, sum of numerators)
+  float* part_acc;
+  float* part_ml;
+  void* out;           // [T,Bq,Hq,D]
+  int out_f32, f16;
+  int* status;         // device word that is set when a bounded wait gave up
+};
+constexpr int ROWS_TILE = 128;
+
+// The splits' partials of each row, and the row's result over other tokens where there is one (own: that result in fp32,
+// own_lse: its denominator as in DecodeParams), joined into out.  A row without tokens becomes zero.
+struct JoinParams {
+  long long rows;
+  int D, ns;
+  const float* part_acc;
+  const float* part_ml;
+  const float* own;      // [rows,D] or null
+  const float* own_lse;  // [rows]
+  void* out;
+  int out_f32, f16;
+};
+
+// Copies sequences of one cache to another one, or within one (xq_gather.cu).
+constexpr int GATHER_MAX_LAYERS = 32;
+struct GatherLayer {
+  uint32_t src[6], dst[6];  // the regions' offsets in the workspaces, in units of 256 bytes
+  int n_q, r;               // tokens: packed, window
+  int bk, bv;               // code bits; 0: the layer has no codes of its own
+};
+struct GatherParams {
+  const uint8_t* src;
+  uint8_t* dst;
+  const int* index;       // [B_dst]: the source of each sequence
+  int B_src, B_dst, Hkv, D, g, NG, R;
+  int src_cap, dst_cap;   // nq_cap of the two
+  int n_layers;
+  int* status;            // device word that is set when an index is out of range
+  GatherLayer layer[GATHER_MAX_LAYERS];
 };
 
 // Part `part` of `parts` nearly equal shares of n items: [lo, hi), sizes differ by at most one.
@@ -198,5 +258,9 @@ MmaShape decode_mma64_shape_t(int g, int bk, int bv);
 template <int D>
 cudaError_t launch_chunk_t(const ChunkParams& p, cudaStream_t st);
 cudaError_t launch_merge(const MergeParams& p, cudaStream_t st);
+cudaError_t launch_rows_generic(const RowsParams& p, cudaStream_t st);
+cudaError_t launch_join(const JoinParams& p, cudaStream_t st);
+cudaError_t launch_gather(const GatherParams& p, cudaStream_t st);
+int gather_place_limit();  // sequences of a cache that can be reordered in place
 
 }  // namespace xq
