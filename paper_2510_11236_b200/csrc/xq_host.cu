@@ -1096,7 +1096,8 @@ int launch_rows(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, i
   cudaError_t e;
   {
     Timer t(c, st, 0);
-    e = launch_rows_generic(p, st);
+    if (c->cfg.kernel == XQ_KERNEL_GENERIC) e = launch_rows_generic(p, st);
+    else e = dm.D == 128 ? launch_rows_t<128>(p, st) : launch_rows_t<64>(p, st);
   }
   c->launches++;
   return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
@@ -1170,8 +1171,10 @@ int prefix_impl(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* o
     rc = chunk_impl(c, layer, q, own, T, 1, stream, lse);
     if (rc != XQ_OK) return rc;
   }
-  rc = launch_rows(c, prefix, layer, plan, T, ns, nullptr, q, out, out_f32, acc, ml, st);
-  if (rc != XQ_OK) return rc;
+  // (one split of the prefix alone: the kernel writes the result)
+  const bool direct = ns == 1 && S == 0 && c->cfg.kernel != XQ_KERNEL_GENERIC;
+  rc = launch_rows(c, prefix, layer, plan, T, ns, nullptr, q, out, out_f32, direct ? nullptr : acc, ml, st);
+  if (rc != XQ_OK || direct) return rc;
   return launch_rows_join(c, plan, ns, acc, ml, own, lse, out, out_f32, st);
 }
 
@@ -1196,8 +1199,9 @@ int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const in
   if (rc != XQ_OK) return rc;
   uint8_t* w = (uint8_t*)workspace;
   float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml);
-  rc = launch_rows(c, c, layer, plan, T, ns, lengths, q, out, out_f32, acc, ml, st);
-  if (rc != XQ_OK) return rc;
+  const bool direct = ns == 1 && c->cfg.kernel != XQ_KERNEL_GENERIC;
+  rc = launch_rows(c, c, layer, plan, T, ns, lengths, q, out, out_f32, direct ? nullptr : acc, ml, st);
+  if (rc != XQ_OK || direct) return rc;
   return launch_rows_join(c, plan, ns, acc, ml, nullptr, nullptr, out, out_f32, st);
 }
 

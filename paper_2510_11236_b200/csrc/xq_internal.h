@@ -174,7 +174,7 @@ struct RowsParams {
 };
 constexpr int ROWS_TILE = 128;
 
-// The splits' partials of each row, and the row's result over other tokens where there is one (own: that result in fp32,
+// The splits' partials of each row (one whose reference is -infinity has no sums), and the row's result over other tokens where there is one (own: that result in fp32,
 // own_lse: its denominator as in DecodeParams), joined into out.  A row without tokens becomes zero.
 struct JoinParams {
   long long rows;
@@ -258,6 +258,8 @@ MmaShape decode_mma64_shape_t(int g, int bk, int bv);
 template <int D>
 cudaError_t launch_chunk_t(const ChunkParams& p, cudaStream_t st);
 cudaError_t launch_merge(const MergeParams& p, cudaStream_t st);
+template <int D>
+cudaError_t launch_rows_t(const RowsParams& p, cudaStream_t st);
 cudaError_t launch_rows_generic(const RowsParams& p, cudaStream_t st);
 cudaError_t launch_join(const JoinParams& p, cudaStream_t st);
 cudaError_t launch_gather(const GatherParams& p, cudaStream_t st);

@@ -102,10 +102,11 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
 #pragma unroll
   for (int j = 0; j < DPL; ++j) a[j] = 0.f;
   auto add = [&](float m, float l, const float* v) {
-    const float f = m == -CUDART_INF_F ? 0.f : exp2f(m - M);
-    L = fmaf(l, f, L);
+    const bool none = m == -CUDART_INF_F;  // v is then not defined
+    const float f = exp2f(m - M);
+    L = none ? L : fmaf(l, f, L);
 #pragma unroll
-    for (int j = 0; j < DPL; ++j) a[j] = fmaf(v[j], f, a[j]);
+    for (int j = 0; j < DPL; ++j) a[j] = none ? a[j] : fmaf(v[j], f, a[j]);
   };
 #pragma unroll 4
   for (int s = 0; s < p.ns; ++s) {
