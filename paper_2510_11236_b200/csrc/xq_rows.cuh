@@ -6,8 +6,8 @@
 // 2 s, is a half-precision number when s is (1-bit codes: s c + z).  The rest does not depend on the token (keys: within a
 // group of tokens) or on the channel (values: within a group of channels), so it is a few more rows of the same operand:
 //
-//   S = Q [s (c - 1) | z, s of the tile's token groups]           64 + 16 columns, fp32
-//   O += P [s (c - 1) | z, s of the channel groups | 1]           head_dim + 16 columns, fp32; the last one sums P
+//   S = Q [s (c - 1) | z, s of the token groups]                 128 + 16 columns, fp32
+//   O += P [s (c - 1) | z, s of the channel groups | 1]          head_dim + 16 columns, fp32; the last one sums P
 //
 // Q: half precision, scaled by a power of two for each row (exact for bfloat16 down to 2^-16 of the row's largest element);
 // P: the softmax numerators times 2^R_PEXP, rounded to half precision (2^-12 of each on average; the result is divided by the
@@ -15,11 +15,12 @@
 // codes and numerators, as the chunk kernel has them, that is 608 in place of 1280 cycles of the tensor pipe a tile, and half
 // the expansion.
 //
-// Eight softmax warps share a tile of 128 tokens: a thread has a row (= lane of tensor memory) and half of the tokens, P takes
-// the columns of its S, and with two S the products of the next tile run meanwhile.  The softmax reference of a row is raised
-// only when a logit exceeds it by R_TAU (log2 units): one barrier with a vote a tile, an exchange of the halves' maxima and a
-// pass over O where the vote says so.  Eight warps expand (four keys, four values), one issues products, one copies packed
-// data.  Window tokens go into the same operands as they are, bfloat16 ones scaled by a power of two for each tile.
+// Tokens go in batches of 128, two tiles each.  Two groups of four softmax warps (thread = row = lane of tensor memory) take
+// the first and the second tiles; with two S the products run a batch ahead, and one group can compute exponentials while the
+// other reads and searches its S.  The softmax reference of a row is passed from one group to the other in the order of the
+// tiles, before the exponentials, and is raised only when a logit exceeds it by R_TAU (log2 units), which takes a pass over O.
+// P takes columns of its S.  Eight warps expand (four keys, four values), one issues products, one copies packed data.  Window
+// tokens go into the same operands as they are, bfloat16 ones scaled by a power of two for each batch.
 //
 // Every wait on an mbarrier is bounded, as in the chunk kernel: a thread that gives up sets a flag that ends the others' waits,
 // and the CTA reports through the status word.
@@ -31,13 +32,15 @@
 namespace xq {
 namespace {
 
-constexpr int RT = XQ_BATCH;     // tokens of a tile
-constexpr int R_BUFS = 2;        // expanded tiles of keys, of values
-constexpr int R_RAW = 3;         // packed tiles in flight
+constexpr int RB = XQ_BATCH;     // tokens of a batch
+constexpr int RT = 64;           // of a tile, half a batch
+constexpr int R_BUFS = 2;        // expanded batches of keys, of values
+constexpr int R_RAW = 4;         // packed batches in flight
 constexpr float R_TAU = 8.f;
 constexpr int R_PEXP = 7;        // numerators are at most 2^(R_PEXP + R_TAU) as fp16
+constexpr int R_EXPAND = 4;      // expanding warps of a kind: keys 8 .. 11, values 12 .. 15
 constexpr int R_MMA = 16, R_LOAD = 17, R_THREADS = 18 * 32;
-constexpr int R_UNITS = 4;       // window tiles whose exponents are kept
+constexpr int R_UNITS = 4;       // window batches whose exponents are kept
 constexpr uint32_t MAX_DOUBLED = 0x77ff;  // the largest half-precision number whose double is finite
 
 // shared-memory matrix descriptor, K-major, 128-byte swizzle: rows of 128 bytes, groups of eight 1024 bytes apart
@@ -77,27 +80,28 @@ __device__ __forceinline__ float2 halves_of(uint64_t a) {
   asm("mov.b64 {%0, %1}, %2;\n" : "=f"(d.x), "=f"(d.y) : "l"(a));
   return d;
 }
-// Barrier of the softmax warps, and one with a vote: whether any thread's predicate is set.  A named barrier has no limit, so
-// all of them come to the same ones whatever fails: they leave their loop by a vote alone.
+// barrier of the softmax warps
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }
-__device__ __forceinline__ bool softmax_any(bool p) {
-  uint32_t any;
-  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbar.red.or.pred q, 1, 256, p;\nselp.u32 %0, 1, 0, q;\n}\n"
-               : "=r"(any) : "r"((uint32_t)p) : "memory");
-  return any != 0u;
+// A warp's bounded wait.  What follows when the first look fails is out of line: most looks do not, and the kernel's roles
+// share an instruction cache.
+__device__ __noinline__ bool warp_wait_longer(uint32_t bar, uint32_t parity, volatile int* dead) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, dead));
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) != 0u) || warp_wait_longer(bar, parity, dead);
 }
 
 template <int D, int BK, int BV, int GS>
 struct RowsLayout {
   static constexpr int NG = D / GS;
   static constexpr int KROW = D * BK / 8;              // packed bytes of a token's keys
-  static constexpr int KN = RT + 16, VN = D + 16;      // rows of the operands (N of the products)
+  static constexpr int KN = RB + 16, VN = D + 16;      // rows of the operands: tokens and 16 more, channels and 16 more
   // an operand: blocks of 128-byte rows (64 channels of the keys, 64 tokens of the values)
-  static constexpr int KBLOCK = KN * 128, KBYTES = D / 64 * KBLOCK, VBLOCK = VN * 128, VBYTES = RT / 64 * VBLOCK;
+  static constexpr int KBLOCK = KN * 128, KBYTES = D / 64 * KBLOCK, VBLOCK = VN * 128, VBYTES = RB / 64 * VBLOCK;
   static constexpr int ONES = D + 8;                   // the operand row, and column of O, that sums P
-  // a raw stage: key codes, key parameters, value codes, value parameters of a tile
-  static constexpr int RAW_KM = RT * KROW, RAW_VC = RAW_KM + RT / GS * 4 * D, RAW_VM = RAW_VC + 16 * D * BV;
-  static constexpr int RAW = RAW_VM + RT * 4 * NG;
+  // a raw stage: key codes, key parameters, value codes, value parameters of a batch
+  static constexpr int RAW_KM = RB * KROW, RAW_VC = RAW_KM + RB / GS * 4 * D, RAW_VM = RAW_VC + 16 * D * BV;
+  static constexpr int RAW = RAW_VM + RB * 4 * NG;
   static constexpr int OFF_V = R_BUFS * KBYTES, OFF_RAW = OFF_V + R_BUFS * VBYTES, TOTAL = OFF_RAW + R_RAW * RAW;
   static_assert(KBLOCK % 1024 == 0 && VBLOCK % 1024 == 0 && RAW % 16 == 0, "alignment");
   static_assert(TOTAL + 1024 <= 226 * 1024, "shared memory");
@@ -166,9 +170,9 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   using Ly = RowsLayout<D, BK, BV, GS>;
   constexpr int NG = Ly::NG;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 3 * 2 + 2 * R_UNITS + 2];
-  __shared__ float half_sm[2][ROWS_TILE];    // what the two threads of a row tell each other
-  __shared__ uint32_t unit_sm[R_UNITS][2][4];  // window tile, keys / values: largest magnitude of each expanding warp
+  __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 2 + 2 * 4 + 8 + 2 * R_UNITS + 2];
+  __shared__ float half_sm[2][ROWS_TILE], m_sm[ROWS_TILE];  // largest element of half a row of q; softmax reference
+  __shared__ uint32_t unit_sm[R_UNITS][2][R_EXPAND];        // window batch, keys / values: largest magnitude of each expanding warp
   __shared__ uint32_t tmem_base_sm;
   __shared__ volatile int dead_sm;
 
@@ -176,16 +180,17 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t sm = ((uint32_t)__cvta_generic_to_shared(smem_raw) + 1023u) & ~1023u;
   const uint32_t bars = (uint32_t)__cvta_generic_to_shared(&bar_mem[0]);
-  const uint32_t bar_rfull = bars;                       // [R_RAW] a tile's packed data is there
+  const uint32_t bar_rfull = bars;                       // [R_RAW] a batch's packed data is there
   const uint32_t bar_rfree = bar_rfull + 8 * R_RAW;      // [R_RAW] all expanding warps are done with it
-  const uint32_t bar_kfull = bar_rfree + 8 * R_RAW;      // [R_BUFS] a tile's keys are expanded
+  const uint32_t bar_kfull = bar_rfree + 8 * R_RAW;      // [R_BUFS] a batch's keys are expanded
   const uint32_t bar_kfree = bar_kfull + 8 * R_BUFS;     // [R_BUFS] their products are complete
   const uint32_t bar_vfull = bar_kfree + 8 * R_BUFS;     // [R_BUFS] the same of the values
   const uint32_t bar_vfree = bar_vfull + 8 * R_BUFS;     // [R_BUFS]
-  const uint32_t bar_s = bar_vfree + 8 * R_BUFS;         // [2] S of a tile is complete
-  const uint32_t bar_p = bar_s + 16;                     // [2] its numerators are written
-  const uint32_t bar_o = bar_p + 16;                     // [2] its value products are complete
-  const uint32_t bar_kunit = bar_o + 16;                 // [R_UNITS] the magnitudes of a window tile's keys are known
+  const uint32_t bar_s = bar_vfree + 8 * R_BUFS;         // [2] S of a batch is complete
+  const uint32_t bar_p = bar_s + 16;                     // [2][2] the numerators of a batch's first / second tile are written
+  const uint32_t bar_o = bar_p + 32;                     // [2][2] its value products are complete
+  const uint32_t bar_turn = bar_o + 32;                  // [4 warps][2] the reference for a first / second tile is there
+  const uint32_t bar_kunit = bar_turn + 64;              // [R_UNITS] the magnitudes of a window batch's keys are known
   const uint32_t bar_vunit = bar_kunit + 8 * R_UNITS;    // [R_UNITS] the same of its values
   const uint32_t bar_q = bar_vunit + 8 * R_UNITS;        // Q is written
   const uint32_t bar_end = bar_q + 8;                    // every product is complete
@@ -194,25 +199,28 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
 #pragma unroll
     for (int i = 0; i < R_RAW; ++i) {
       mbar_init(bar_rfull + 8 * i, 1);
-      mbar_init(bar_rfree + 8 * i, 8);
+      mbar_init(bar_rfree + 8 * i, 2 * R_EXPAND);
     }
 #pragma unroll
     for (int i = 0; i < R_BUFS; ++i) {
-      mbar_init(bar_kfull + 8 * i, 4);
+      mbar_init(bar_kfull + 8 * i, R_EXPAND);
       mbar_init(bar_kfree + 8 * i, 1);
-      mbar_init(bar_vfull + 8 * i, 4);
+      mbar_init(bar_vfull + 8 * i, R_EXPAND);
       mbar_init(bar_vfree + 8 * i, 1);
     }
+    mbar_init(bar_s, 1);
+    mbar_init(bar_s + 8, 1);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(bar_s + 8 * i, 1);
-      mbar_init(bar_p + 8 * i, 8);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar_p + 8 * i, 4);
       mbar_init(bar_o + 8 * i, 1);
+      mbar_init(bar_turn + 16 * i, 1);
+      mbar_init(bar_turn + 16 * i + 8, 1);
     }
 #pragma unroll
     for (int i = 0; i < R_UNITS; ++i) {
-      mbar_init(bar_kunit + 8 * i, 4);
-      mbar_init(bar_vunit + 8 * i, 4);
+      mbar_init(bar_kunit + 8 * i, R_EXPAND);
+      mbar_init(bar_vunit + 8 * i, R_EXPAND);
     }
     mbar_init(bar_q, 8);
     mbar_init(bar_end, 1);
@@ -224,7 +232,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   grid_dependents_go();
   if (warp == R_MMA) tmem_alloc((uint32_t)__cvta_generic_to_shared(&tmem_base_sm), 512u);
 
-  // ---- the CTA's rows and tiles ----
+  // ---- the CTA's rows and batches ----
   const int G = dm.G;
   const int split = blockIdx.x % p.ns, rest = blockIdx.x / p.ns, rt = rest % p.row_tiles, bh = rest / p.row_tiles;
   const int u = bh / dm.Hkv, hk = bh - u * dm.Hkv;
@@ -235,19 +243,22 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     n_q = min(n_q, S);
     r = S - n_q;
   }
-  const int pk_tiles = (n_q + RT - 1) / RT, all_tiles = pk_tiles + (r + RT - 1) / RT;
+  const int pk_batches = (n_q + RB - 1) / RB, all_batches = pk_batches + (r + RB - 1) / RB;
   int t_lo, t_hi;
-  share_of(all_tiles, p.ns, split, t_lo, t_hi);
+  share_of(all_batches, p.ns, split, t_lo, t_hi);
   const int N = t_hi - t_lo;
-  const int n_pk = max(0, min(t_hi, pk_tiles) - t_lo);  // packed tiles of the range; window tile i is the (i - n_pk)-th one
-  auto call_row = [&](int k) {                          // of the stream's row row0 + k
+  const int n_pk = max(0, min(t_hi, pk_batches) - t_lo);  // packed batches of the range; batch i is window batch i - n_pk
+  auto call_row = [&](int k) {                            // of the stream's row row0 + k
     const int x = row0 + k, h = x % G, ji = x / G, i = ji % p.each, j = ji / p.each;
     return ((size_t)j * (dm.B * p.each) + (size_t)u * p.each + i) * dm.Hq + hk * G + h;
   };
-  // exponent of a window tile's keys (0) or values (1)
-  auto tile_exponent = [&](int i, int which) {
+  // exponent of a window batch's keys (0) or values (1)
+  auto batch_exponent = [&](int i, int which) {
     const uint32_t* m = unit_sm[(i - n_pk) % R_UNITS][which];
-    return p.f16 ? 0 : window_exponent(bf16_top(max(max(m[0], m[1]), max(m[2], m[3]))));
+    uint32_t x = 0u;
+#pragma unroll
+    for (int k = 0; k < R_EXPAND; ++k) x = max(x, m[k]);
+    return p.f16 ? 0 : window_exponent(bf16_top(x));
   };
 
   tc_fence_before();
@@ -259,39 +270,41 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     // ================= products: the loop is warp-uniform, one elected lane issues =================
     constexpr uint32_t IDK = rows_idesc(Ly::KN), IDV = rows_idesc(Ly::VN);
     const uint32_t tb = __shfl_sync(0xffffffffu, tbase, 0), smu = __shfl_sync(0xffffffffu, sm, 0);
-    bool ok = __all_sync(0xffffffffu, mbar_wait(bar_q, 0, &dead_sm));
-    // values of tile i - 2, then keys of tile i, whose S takes the place of that tile's numerators
+    bool ok = warp_wait(bar_q, 0, &dead_sm);
+    // values of batch i - 2, a tile at a time, then keys of batch i, whose S takes the place of those numerators
 #pragma unroll 1
     for (int i = 0; ok && i < N + 2; ++i) {
+      const int b = i & 1;
+      const uint32_t turn = ((i >> 1) & 1) ^ 1;  // of what belongs to batch i - 2
+      const uint32_t dS = tb + Ly::COL_S + b * Ly::KN;
       if (i >= 2) {
-        const int j = i - 2;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_vfull + 8 * (j % R_BUFS), (j / R_BUFS) & 1, &dead_sm) &&
-                                         mbar_wait(bar_p + 8 * (j & 1), (j >> 1) & 1, &dead_sm));
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t pt = tb + Ly::COL_S + (j & 1) * Ly::KN;
-          const uint64_t v = rows_desc(smu + Ly::OFF_V + (j % R_BUFS) * Ly::VBYTES);
+        ok = warp_wait(bar_vfull + 8 * b, turn, &dead_sm);
+#pragma unroll 1
+        for (int g = 0; ok && g < 2; ++g) {
+          ok = warp_wait(bar_p + 16 * b + 8 * g, turn, &dead_sm);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t v = rows_desc(smu + Ly::OFF_V + b * Ly::VBYTES + g * Ly::VBLOCK);
 #pragma unroll
-          for (int ks = 0; ks < RT / 16; ++ks)
-            rows_mma(tb + Ly::COL_O, pt + 8 * ks, v + (ks / 4) * (Ly::VBLOCK / 16) + 2 * (ks % 4), IDV, j > 0 || ks > 0);
-          rows_commit(bar_vfree + 8 * (j % R_BUFS));
-          rows_commit(bar_o + 8 * (j & 1));
+            for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, dS + g * RT + 8 * ks, v + 2 * ks, IDV, i > 2 || g > 0 || ks > 0);
+            rows_commit(bar_o + 16 * b + 8 * g);
+            if (g == 1) rows_commit(bar_vfree + 8 * b);
+          }
+          __syncwarp();
         }
-        __syncwarp();
+        if (!ok) break;
       }
       if (i < N) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_kfull + 8 * (i % R_BUFS), (i / R_BUFS) & 1, &dead_sm));
+        ok = warp_wait(bar_kfull + 8 * b, (i >> 1) & 1, &dead_sm);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint32_t dS = tb + Ly::COL_S + (i & 1) * Ly::KN;
-          const uint64_t k = rows_desc(smu + (i % R_BUFS) * Ly::KBYTES);
+          const uint64_t k = rows_desc(smu + b * Ly::KBYTES);
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks)
-            rows_mma(dS, tb + Ly::COL_Q + 8 * ks, k + (ks / 4) * (Ly::KBLOCK / 16) + 2 * (ks % 4), IDK, ks > 0);
-          rows_commit(bar_s + 8 * (i & 1));
-          rows_commit(bar_kfree + 8 * (i % R_BUFS));
+          for (int ks = 0; ks < D / 16; ++ks) rows_mma(dS, tb + Ly::COL_Q + 8 * ks, k + (ks / 4) * (Ly::KBLOCK / 16) + 2 * (ks % 4), IDK, ks > 0);
+          rows_commit(bar_s + 8 * b);
+          rows_commit(bar_kfree + 8 * b);
         }
         __syncwarp();
       }
@@ -302,29 +315,29 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     }
     __syncwarp();
   } else if (warp == R_LOAD) {
-    // ================= packed data, a tile at a time =================
+    // ================= packed data, a batch at a time =================
     if (lane == 0) {
       const size_t first = (size_t)t_lo;
-      const uint8_t* const kc = reinterpret_cast<const uint8_t*>(p.L.k_codes) + (size_t)bh * ((size_t)dm.nq_cap * Ly::KROW) + first * (RT * Ly::KROW);
+      const uint8_t* const kc = reinterpret_cast<const uint8_t*>(p.L.k_codes) + (size_t)bh * ((size_t)dm.nq_cap * Ly::KROW) + first * (RB * Ly::KROW);
       const uint8_t* const vc = reinterpret_cast<const uint8_t*>(p.L.v_codes) + (size_t)bh * ((size_t)dm.nq_cap * (D * BV / 8)) + first * (16 * D * BV);
-      const uint8_t* const km = reinterpret_cast<const uint8_t*>(p.L.k_meta) + (size_t)bh * ((size_t)(dm.nq_cap / GS) * (4 * D)) + first * (RT / GS * 4 * D);
-      const uint8_t* const vm = reinterpret_cast<const uint8_t*>(p.L.v_meta) + (size_t)bh * ((size_t)dm.nq_cap * 4 * NG) + first * (RT * 4 * NG);
+      const uint8_t* const km = reinterpret_cast<const uint8_t*>(p.L.k_meta) + (size_t)bh * ((size_t)(dm.nq_cap / GS) * (4 * D)) + first * (RB / GS * 4 * D);
+      const uint8_t* const vm = reinterpret_cast<const uint8_t*>(p.L.v_meta) + (size_t)bh * ((size_t)dm.nq_cap * 4 * NG) + first * (RB * 4 * NG);
       int i = 0;
       for (; i < n_pk; ++i) {
         if (i >= R_RAW && !mbar_wait(bar_rfree + 8 * (i % R_RAW), (i / R_RAW - 1) & 1, &dead_sm)) break;
         const uint32_t dst = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW, bar = bar_rfull + 8 * (i % R_RAW);
         mbar_expect_tx(bar, Ly::RAW);
-        bulk_load(dst, kc + (size_t)i * (RT * Ly::KROW), RT * Ly::KROW, bar);
-        bulk_load(dst + Ly::RAW_KM, km + (size_t)i * (RT / GS * 4 * D), RT / GS * 4 * D, bar);
+        bulk_load(dst, kc + (size_t)i * (RB * Ly::KROW), RB * Ly::KROW, bar);
+        bulk_load(dst + Ly::RAW_KM, km + (size_t)i * (RB / GS * 4 * D), RB / GS * 4 * D, bar);
         bulk_load(dst + Ly::RAW_VC, vc + (size_t)i * (16 * D * BV), 16 * D * BV, bar);
-        bulk_load(dst + Ly::RAW_VM, vm + (size_t)i * (RT * 4 * NG), RT * 4 * NG, bar);
+        bulk_load(dst + Ly::RAW_VM, vm + (size_t)i * (RB * 4 * NG), RB * 4 * NG, bar);
       }
       // no copy may be in flight when the shared memory is released (nobody may have waited for them if a wait gave up)
       for (int k = max(0, i - R_RAW); k < i; ++k)
         for (int n = 0; n < WAIT_LIMIT && !mbar_try_wait(bar_rfull + 8 * (k % R_RAW), (k / R_RAW) & 1); ++n) {}
     } else if (N > n_pk) {
       // window rows of the range: into L2 before the expanding warps come to them
-      const int w_lo = (t_lo + n_pk - pk_tiles) * RT, w_hi = min(r, (t_hi - pk_tiles) * RT);
+      const int w_lo = (t_lo + n_pk - pk_batches) * RB, w_hi = min(r, (t_hi - pk_batches) * RB);
       const char* wk = reinterpret_cast<const char*>(p.L.win_k + ((size_t)bh * dm.R + w_lo) * D);
       const char* wv = reinterpret_cast<const char*>(p.L.win_v + ((size_t)bh * dm.R + w_lo) * D);
       for (int x = (lane - 1) * 128; x < (w_hi - w_lo) * 2 * D; x += 31 * 128) {
@@ -337,138 +350,148 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     // ================= expansion: keys (warps 8 .. 11), values (12 .. 15) =================
     const int ew = warp & 3, o = lane & 3, sub = lane >> 2;  // a lane's sixteen elements of 64, and its row of eight
     const bool keys = warp < 12;
-    // keys: 64 channels from 64 kb on, of the token groups ("slots" of 32 tokens) slot0 .. slot0 + SLOTS - 1
-    constexpr int SLOTS = D / 64;
+    // Keys: 64 channels from 64 kb on of the 32 tokens of each of the slots slot0 .. slot0 + PARTS - 1.  Values: D / 4 channels
+    // from v_c0 on, all of one channel group, of the tokens of either half of the batch.
+    constexpr int PARTS = D / 64, STEPS = D / 32;
     const int kb = D == 128 ? ew & 1 : 0, slot0 = D == 128 ? ew & 2 : ew;
-    // values: D / 4 channels from v_c0 on, all of one channel group
     const int v_c0 = ew * (D / 4), vg = v_c0 / GS;
-    if (!keys && ew == 0) {  // the row that sums the numerators
-      if (lane < 16)
-        for (int b = 0; b < R_BUFS; ++b)
-          sts128(sm + Ly::OFF_V + b * Ly::VBYTES + (lane >> 3) * Ly::VBLOCK + piece_at(Ly::ONES, lane & 7), 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
+    const int rz = keys ? RB + 2 * slot0 : D + vg, rs = keys ? rz + 1 : rz + NG;  // operand rows of the zero-points and of the scales
+    const int row = keys ? 32 * slot0 + sub : v_c0 + sub;
+    const int shift = ((keys ? BK : BV) == 2 ? 0 : 4) * (o & 1);
+    constexpr int PERK = 32 / BK, CB = Ly::KROW < 16 ? Ly::KROW : 16;
+    const int word = (64 * kb + 16 * o) / PERK;
+    // what a lane reads, from the raw stage's start, and writes, from the operand's
+    const uint32_t code_off = keys ? slot0 * (32 * Ly::KROW) + word * 4 / CB * (32 * CB) + word * 4 % CB + sub * CB
+                                   : Ly::RAW_VC + (BV == 2 ? o * 4 : o / 2 * 4) + (v_c0 + sub) * 16;
+    const uint32_t meta_off = keys ? Ly::RAW_KM + 2 * (lane * (D / 32) + 2 * kb) : Ly::RAW_VM + lane * (4 * NG) + 2 * vg;
+    const uint32_t op_off = keys ? kb * Ly::KBLOCK : Ly::OFF_V;
+    if (!keys && ew < 2 && lane < 8) {  // the row that sums the numerators
+      for (int b = 0; b < R_BUFS; ++b)
+        sts128(sm + Ly::OFF_V + b * Ly::VBYTES + ew * Ly::VBLOCK + piece_at(Ly::ONES, lane), 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
       proxy_fence();
     }
+    __syncwarp();
 #pragma unroll 1
     for (int i = 0; i < N; ++i) {
-      const int t = t_lo + i, b = i % R_BUFS;
+      const int b = i & 1;
       const bool packed = i < n_pk;
-      bool ok = !packed || mbar_wait(bar_rfull + 8 * (i % R_RAW), (i / R_RAW) & 1, &dead_sm);
-      ok = ok && (i < R_BUFS || mbar_wait((keys ? bar_kfree : bar_vfree) + 8 * b, (i / R_BUFS - 1) & 1, &dead_sm));
-      if (!__all_sync(0xffffffffu, ok)) break;
+      if (packed && !warp_wait(bar_rfull + 8 * (i % R_RAW), (i / R_RAW) & 1, &dead_sm)) break;
+      if (i >= R_BUFS && !warp_wait((keys ? bar_kfree : bar_vfree) + 8 * b, ((i >> 1) & 1) ^ 1, &dead_sm)) break;
       const uint32_t raw = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW;
+      const uint32_t dst = sm + op_off + b * (keys ? Ly::KBYTES : Ly::VBYTES);
       if (packed && keys) {
-        const uint32_t dst = sm + b * Ly::KBYTES + kb * Ly::KBLOCK;
-        constexpr int PER = 32 / BK, CB = Ly::KROW < 16 ? Ly::KROW : 16;
-        const int word = (64 * kb + 16 * o) / PER, shift = BK == 2 ? 0 : 4 * (o & 1);
-#pragma unroll
-        for (int x = 0; x < SLOTS; ++x) {
-          const int slot = slot0 + x, rz = RT + 2 * slot, rs = rz + 1;  // operand rows of the zero-points and of the scales
-          const uint32_t src = raw + slot * (32 * Ly::KROW) + word * 4 / CB * (32 * CB) + word * 4 % CB + sub * CB;
-          uint32_t codes[4];  // (loads first: an access to shared memory does not move past another)
+#pragma unroll 1
+        for (int x = 0; x < PARTS; ++x) {
+          const uint32_t src = raw + code_off + x * (32 * Ly::KROW);
+          uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
 #pragma unroll
           for (int k = 0; k < 4; ++k) codes[k] = lds32(src + 8 * k * CB);
           // parameters of channels 64 kb + lane and 32 more, side by side in the group's order
-          const uint32_t meta = raw + Ly::RAW_KM + slot * 32 / GS * (4 * D);
-          uint32_t sw = lds32(meta + 2 * (lane * (D / 32) + 2 * kb)), zw = lds32(meta + 2 * (D + lane * (D / 32) + 2 * kb));
+          const uint32_t meta = raw + meta_off + (slot0 + x) * 32 / GS * (4 * D);
+          uint32_t sw = lds32(meta), zw = lds32(meta + 2 * D);
           const bool large = BK == 2 && __any_sync(0xffffffffu, (sw & 0xffffu) > MAX_DOUBLED || (sw >> 16) > MAX_DOUBLED);
           if (large) sw = zw = 0u;
           const int at = (lane & ~3) | ((lane & 1) << 1) | ((lane >> 1) & 1);  // elements of four: 0, 2, 1, 3
-          sts16(dst + piece_at(rz, at >> 3) + 2 * (at & 7), zw & 0xffffu);
-          sts16(dst + piece_at(rz, 4 + (at >> 3)) + 2 * (at & 7), zw >> 16);
-          sts16(dst + piece_at(rs, at >> 3) + 2 * (at & 7), sw & 0xffffu);
-          sts16(dst + piece_at(rs, 4 + (at >> 3)) + 2 * (at & 7), sw >> 16);
+          const uint32_t to_z = dst + piece_at(rz + 2 * x, at >> 3) + 2 * (at & 7), to_s = dst + piece_at(rs + 2 * x, at >> 3) + 2 * (at & 7);
+          sts16(to_z, zw & 0xffffu);
+          sts16(to_z ^ 64u, zw >> 16);  // four pieces on
+          sts16(to_s, sw & 0xffffu);
+          sts16(to_s ^ 64u, sw >> 16);
           __syncwarp();
-          const uint32_t d0 = dst + piece_at(32 * slot + sub, 2 * o), d1 = dst + piece_at(32 * slot + sub, 2 * o + 1);
+          const uint32_t d0 = dst + piece_at(row + 32 * x, 2 * o), d1 = d0 ^ 16u, s_row = dst + piece_at(rs + 2 * x, 2 * o);
           if (!large) {
-            const uint4 s0 = lds128(dst + piece_at(rs, 2 * o)), s1 = lds128(dst + piece_at(rs, 2 * o + 1));
+            const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
 #pragma unroll
             for (int k = 0; k < 4; ++k) expand16<BK>(codes[k] >> shift, s0, s1, d0 + 1024 * k, d1 + 1024 * k);
           } else {
+            const uint32_t group = raw + Ly::RAW_KM + (slot0 + x) * 32 / GS * (4 * D);
 #pragma unroll 1
             for (int k = 0; k < 8; ++k) {
-              auto s_at = [&](int e) { const int d = 64 * kb + 16 * o + 8 * (k & 1) + e; return meta + 2 * (d % 32 * (D / 32) + d / 32); };
+              auto s_at = [&](int e) { const int d = 64 * kb + 16 * o + 8 * (k & 1) + e; return group + 2 * (d % 32 * (D / 32) + d / 32); };
               restore8<BK>(lds32(src + 8 * (k >> 1) * CB) >> (shift + 2 * BK * (k & 1)), s_at, [&](int e) { return s_at(e) + 2 * D; },
                            (k & 1 ? d1 : d0) + 1024 * (k >> 1));
             }
           }
         }
       } else if (packed) {
-        const int rz = D + vg, rs = D + NG + vg, valid = n_q - t * RT;
+        const int valid = n_q - (t_lo + i) * RB;  // tokens of the batch that exist
+#pragma unroll 1
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t src = raw + code_off + x * (BV == 2 ? D * 16 : 8), block = dst + x * Ly::VBLOCK;
+          uint32_t codes[STEPS];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t dst = sm + Ly::OFF_V + b * Ly::VBYTES + half * Ly::VBLOCK;
-          const int shift = BV == 2 ? 0 : 4 * (o & 1);
-          const uint32_t src = raw + Ly::RAW_VC + (BV == 2 ? half * (D * 16) + o * 4 : (2 * half + o / 2) * 4) + (v_c0 + sub) * 16;
-          uint32_t codes[D / 32];
+          for (int k = 0; k < STEPS; ++k) codes[k] = lds32(src + 128 * k);
+          // Parameters of token `lane` and of lane + 32 of the half, (scale, zero-point); none of tokens that do not exist.  A
+          // word of the operand's rows has tokens (t, t + 2): one of the two lanes writes the scales, the other the zero-points.
+          const uint32_t meta = raw + meta_off + x * (64 * 4 * NG);
+          uint32_t sz[2];
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) codes[k] = lds32(src + 128 * k);
-          // parameters of tokens (ta, ta + 2) of the half, a word of the operand's rows; none of tokens that do not exist
-          const int ta = 64 * half + 4 * (lane >> 1) + (lane & 1);
-          const uint32_t meta = raw + Ly::RAW_VM + ta * (4 * NG) + 2 * vg;
-          uint32_t sw = lds16(meta) | lds16(meta + 8 * NG) << 16, zw = lds16(meta + 2 * NG) | lds16(meta + 10 * NG) << 16;
-          if (valid < RT) {
-            const uint32_t keep = (ta < valid ? 0xffffu : 0u) | (ta + 2 < valid ? 0xffff0000u : 0u);
-            sw &= keep;
-            zw &= keep;
+          for (int k = 0; k < 2; ++k) sz[k] = lds16(meta + k * (128 * NG)) | lds16(meta + k * (128 * NG) + 2 * NG) << 16;
+          if (valid < RB) {
+            if (64 * x + lane >= valid) sz[0] = 0u;
+            if (64 * x + lane + 32 >= valid) sz[1] = 0u;
           }
-          const bool large = BV == 2 && __any_sync(0xffffffffu, (sw & 0xffffu) > MAX_DOUBLED || (sw >> 16) > MAX_DOUBLED);
-          if (large) sw = zw = 0u;
-          const uint32_t at = ((lane >> 1) & 1) * 8 + (lane & 1) * 4;
-          sts32(dst + piece_at(rz, lane >> 2) + at, zw);
-          sts32(dst + piece_at(rs, lane >> 2) + at, sw);
-          __syncwarp();
-          const uint32_t d0 = dst + piece_at(v_c0 + sub, 2 * o), d1 = dst + piece_at(v_c0 + sub, 2 * o + 1);
-          if (!large) {
-            const uint4 s0 = lds128(dst + piece_at(rs, 2 * o)), s1 = lds128(dst + piece_at(rs, 2 * o + 1));
+          const bool large = BV == 2 && __any_sync(0xffffffffu, (sz[0] & 0xffffu) > MAX_DOUBLED || (sz[1] & 0xffffu) > MAX_DOUBLED);
+          const uint32_t to = block + piece_at(lane & 2 ? rz : rs, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) expand16<BV>(codes[k] >> shift, s0, s1, d0 + 1024 * k, d1 + 1024 * k);
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2);
+            const uint32_t w = lane & 2 ? __byte_perm(other, sz[k], 0x7632) : __byte_perm(sz[k], other, 0x5410);
+            sts32(to ^ (64u * k), large ? 0u : w);
+          }
+          __syncwarp();
+          const uint32_t d0 = block + piece_at(row, 2 * o), d1 = d0 ^ 16u, s_row = block + piece_at(rs, 2 * o);
+          if (!large) {
+            const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) expand16<BV>(codes[k] >> shift, s0, s1, d0 + 1024 * k, d1 + 1024 * k);
           } else {
             // (a token that does not exist stands for the last one that does: its numerator is zero)
 #pragma unroll 1
-            for (int k = 0; k < D / 16; ++k) {
-              auto s_at = [&](int e) { return raw + Ly::RAW_VM + min(64 * half + 16 * o + 8 * (k & 1) + e, valid - 1) * (4 * NG) + 2 * vg; };
+            for (int k = 0; k < 2 * STEPS; ++k) {
+              auto s_at = [&](int e) { return raw + Ly::RAW_VM + min(64 * x + 16 * o + 8 * (k & 1) + e, valid - 1) * (4 * NG) + 2 * vg; };
               restore8<BV>(lds32(src + 128 * (k >> 1)) >> (shift + 2 * BV * (k & 1)), s_at, [&](int e) { return s_at(e) + 2 * NG; },
                            (k & 1 ? d1 : d0) + 1024 * (k >> 1));
             }
           }
         }
       } else {
-        // a window tile: the four warps of a kind settle its exponent, then write it
-        const int w0 = (t - pk_tiles) * RT, n_w = min(RT, r - w0), slot = (i - n_pk) % R_UNITS;
+        // a window batch: the warps of a kind settle its exponent, then write it
+        const int w0 = (t_lo + i - pk_batches) * RB, n_w = min(RB, r - w0), slot_w = (i - n_pk) % R_UNITS;
         const uint4* rows = reinterpret_cast<const uint4*>((keys ? p.L.win_k : p.L.win_v) + ((size_t)bh * dm.R + w0) * D);
+        const uint32_t bar_unit = (keys ? bar_kunit : bar_vunit) + 8 * slot_w;
         float f = 1.f;
         if (!p.f16) {
           uint32_t m = 0u;
 #pragma unroll 4
           for (int x = ew * 32 + lane; x < n_w * (D / 8); x += 128) m = top_of(m, rows[x]);
           m = redux_max_u32(max(m & 0xffffu, m >> 16));
-          if (lane == 0) unit_sm[slot][keys ? 0 : 1][ew] = m;
+          if (lane == 0) unit_sm[slot_w][keys ? 0 : 1][ew] = m;
         }
-        const uint32_t bar_unit = (keys ? bar_kunit : bar_vunit) + 8 * slot;
         if (lane == 0) mbar_arrive(bar_unit);
         if (!p.f16) {
-          if (!__all_sync(0xffffffffu, mbar_wait(bar_unit, ((i - n_pk) / R_UNITS) & 1, &dead_sm))) break;
-          f = pow2i(tile_exponent(i, keys ? 0 : 1));
+          if (!warp_wait(bar_unit, ((i - n_pk) / R_UNITS) & 1, &dead_sm)) break;
+          f = pow2i(batch_exponent(i, keys ? 0 : 1));
         }
         if (keys) {
-          // (the extra rows of a window tile's keys are not looked at)
-          const uint32_t dst = sm + b * Ly::KBYTES;
+          // (the extra rows of a window batch's keys are not looked at)
+          const uint32_t to = sm + b * Ly::KBYTES;
 #pragma unroll 4
-          for (int x = ew * 32 + lane; x < RT * (D / 8); x += 128) {
-            const int row = x / (D / 8), c = x % (D / 8);
-            const uint4 v = reorder8(row < n_w ? rows[x] : make_uint4(0u, 0u, 0u, 0u), f, p.f16);
-            sts128(dst + (c >> 3) * Ly::KBLOCK + piece_at(row, c & 7), v.x, v.y, v.z, v.w);
+          for (int x = ew * 32 + lane; x < RB * (D / 8); x += 128) {
+            const int y = x / (D / 8), c = x % (D / 8);
+            const uint4 v = reorder8(y < n_w ? rows[x] : make_uint4(0u, 0u, 0u, 0u), f, p.f16);
+            sts128(to + (c >> 3) * Ly::KBLOCK + piece_at(y, c & 7), v.x, v.y, v.z, v.w);
           }
         } else {
-          const uint32_t dst = sm + Ly::OFF_V + b * Ly::VBYTES;
+          const uint32_t to = sm + Ly::OFF_V + b * Ly::VBYTES;
           const uint32_t* words = reinterpret_cast<const uint32_t*>(rows);
           if (lane < 16) {
-            sts128(dst + (lane >> 3) * Ly::VBLOCK + piece_at(D + vg, lane & 7), 0u, 0u, 0u, 0u);
-            sts128(dst + (lane >> 3) * Ly::VBLOCK + piece_at(D + NG + vg, lane & 7), 0u, 0u, 0u, 0u);
+            sts128(to + piece_at(lane < 8 ? rz : rs, lane & 7), 0u, 0u, 0u, 0u);
+            sts128(to + Ly::VBLOCK + piece_at(lane < 8 ? rz : rs, lane & 7), 0u, 0u, 0u, 0u);
           }
           // eight tokens of two channels: lanes take neighbouring channels of a token
 #pragma unroll 1
-          for (int x = ew * 32 + lane; x < RT / 8 * (D / 2); x += 128) {
+          for (int x = ew * 32 + lane; x < RB / 8 * (D / 2); x += 128) {
             const int c = x % (D / 2), piece = x / (D / 2);
             uint32_t y[8];
 #pragma unroll
@@ -477,7 +500,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             for (int h = 0; h < 2; ++h) {
               const uint4 v = reorder8(make_uint4(__byte_perm(y[0], y[1], h ? 0x7632 : 0x5410), __byte_perm(y[2], y[3], h ? 0x7632 : 0x5410),
                                                   __byte_perm(y[4], y[5], h ? 0x7632 : 0x5410), __byte_perm(y[6], y[7], h ? 0x7632 : 0x5410)), f, p.f16);
-              sts128(dst + (piece >> 3) * Ly::VBLOCK + piece_at(2 * c + h, piece & 7), v.x, v.y, v.z, v.w);
+              sts128(to + (piece >> 3) * Ly::VBLOCK + piece_at(2 * c + h, piece & 7), v.x, v.y, v.z, v.w);
             }
           }
         }
@@ -490,16 +513,16 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       }
     }
   } else {
-    // ================= softmax: thread = row and half h of a tile's tokens =================
-    const int h = warp >> 2, k_row = tid & 127;
-    const uint32_t row_t = tbase + ((uint32_t)((warp & 3) * 32) << 16);
-    const bool idle = 32 * (warp & 3) >= n_rows;  // none of this warp's rows exists
+    // ================= softmax: group g takes tile g of every batch; thread = row =================
+    const int g = warp >> 2, quarter = warp & 3, k_row = tid & 127;
+    const uint32_t row_t = tbase + ((uint32_t)(quarter * 32) << 16);
+    const bool idle = 32 * quarter >= n_rows;  // none of this warp's rows exists
     float cq = p.scale * 1.4426950408889634f;
     {
       // q: half of this thread's row as fp16 in the operands' order, bfloat16 scaled by a power of two into [1, 2), to tensor
       // memory
       const bool real = k_row < n_rows;
-      const uint4* src = reinterpret_cast<const uint4*>(p.q + (real ? call_row(k_row) * D + h * (D / 2) : 0));
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + (real ? call_row(k_row) * D + g * (D / 2) : 0));
       uint4 x[D / 16];
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) x[i] = real ? src[i] : make_uint4(0u, 0u, 0u, 0u);
@@ -508,7 +531,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         uint32_t m = 0u;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) m = top_of(m, x[i]);
-        half_sm[h][k_row] = bf16_top(m);
+        half_sm[g][k_row] = bf16_top(m);
         softmax_sync();
         const float am = fmaxf(half_sm[0][k_row], half_sm[1][k_row]);
         const int e = am > 0.f ? max(-100, min(100, -exponent_of(am))) : 0;
@@ -523,7 +546,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           const uint4 v = reorder8(x[4 * c + i], f, p.f16);
           y[4 * i] = v.x; y[4 * i + 1] = v.y; y[4 * i + 2] = v.z; y[4 * i + 3] = v.w;
         }
-        tmem_st<16>(row_t + Ly::COL_Q + h * (D / 4) + 16 * c, y);
+        tmem_st<16>(row_t + Ly::COL_Q + g * (D / 4) + 16 * c, y);
       }
       tc_wait_st();
       tc_fence_before();
@@ -532,28 +555,28 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     }
     float m = -CUDART_INF_F;
     int ev = 0;  // exponent of the values in O
-    bool ok = true;
 #pragma unroll 1
     for (int i = 0; i < N; ++i) {
       const bool packed = i < n_pk;
-      bool here = mbar_wait(bar_s + 8 * (i & 1), (i >> 1) & 1, &dead_sm);
+      const int b = i & 1;
+      const uint32_t turn = (i >> 1) & 1;
+      if (!warp_wait(bar_s + 8 * b, turn, &dead_sm)) break;
       if (!packed) {
-        const int slot = (i - n_pk) % R_UNITS, turn = ((i - n_pk) / R_UNITS) & 1;
-        here = here && mbar_wait(bar_kunit + 8 * slot, turn, &dead_sm) && mbar_wait(bar_vunit + 8 * slot, turn, &dead_sm);
+        const int slot = (i - n_pk) % R_UNITS, round = ((i - n_pk) / R_UNITS) & 1;
+        if (!warp_wait(bar_kunit + 8 * slot, round, &dead_sm) || !warp_wait(bar_vunit + 8 * slot, round, &dead_sm)) break;
       }
-      ok = __all_sync(0xffffffffu, here) && ok;
       tc_fence_after();
-      const uint32_t s_t = row_t + Ly::COL_S + (i & 1) * Ly::KN;
+      const uint32_t s_t = row_t + Ly::COL_S + b * Ly::KN + g * RT;
+      const int n_valid = (packed ? n_q - (t_lo + i) * RB : r - (t_lo + i - pk_batches) * RB) - RT * g;  // of this tile
       uint32_t s[2][32];
       float c = cq, bias[2] = {0.f, 0.f}, xm = -CUDART_INF_F;
-      if (ok && !idle) {
+      if (!idle) {
         uint32_t e[8];
-        tmem_ld<32>(s_t + 64 * h, s[0]);
-        tmem_ld<32>(s_t + 64 * h + 32, s[1]);
-        tmem_ld<8>(s_t + RT, e);
+        tmem_ld<32>(s_t, s[0]);
+        tmem_ld<32>(s_t + 32, s[1]);
+        tmem_ld<8>(row_t + Ly::COL_S + b * Ly::KN + RB, e);
         tc_wait_ld();
-        const int n_valid = (packed ? n_q - (t_lo + i) * RT : r - (t_lo + i - pk_tiles) * RT) - 64 * h;  // of this half
-        if (n_valid < 64) {
+        if (n_valid < RT) {
 #pragma unroll
           for (int k = 0; k < 64; ++k)
             if (k >= n_valid) s[k >> 5][k & 31] = 0xff800000u;
@@ -561,45 +584,45 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         // logits in log2 units: S c + bias of their 32 tokens
         if (packed) {
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const uint32_t z = h ? e[4 + 2 * g] : e[2 * g], y = h ? e[5 + 2 * g] : e[2 * g + 1];
-            if (32 * g < n_valid) bias[g] = (__uint_as_float(z) + (BK == 2 ? __uint_as_float(y) : 0.f)) * cq;
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t z = g ? e[4 + 2 * x] : e[2 * x], y = g ? e[5 + 2 * x] : e[2 * x + 1];
+            if (32 * x < n_valid) bias[x] = (__uint_as_float(z) + (BK == 2 ? __uint_as_float(y) : 0.f)) * cq;
           }
         } else {
-          c *= pow2i(-tile_exponent(i, 0));
+          c *= pow2i(-batch_exponent(i, 0));
         }
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          float a = __uint_as_float(s[g][0]), d = __uint_as_float(s[g][1]);
+        for (int x = 0; x < 2; ++x) {
+          float a = __uint_as_float(s[x][0]), d = __uint_as_float(s[x][1]);
 #pragma unroll
           for (int k = 2; k < 30; k += 4) {
-            a = fmaxf(fmaxf(a, __uint_as_float(s[g][k])), __uint_as_float(s[g][k + 1]));
-            d = fmaxf(fmaxf(d, __uint_as_float(s[g][k + 2])), __uint_as_float(s[g][k + 3]));
+            a = fmaxf(fmaxf(a, __uint_as_float(s[x][k])), __uint_as_float(s[x][k + 1]));
+            d = fmaxf(fmaxf(d, __uint_as_float(s[x][k + 2])), __uint_as_float(s[x][k + 3]));
           }
-          a = fmaxf(fmaxf(a, __uint_as_float(s[g][30])), __uint_as_float(s[g][31]));
-          xm = fmaxf(xm, fmaf(fmaxf(a, d), c, bias[g]));
+          a = fmaxf(fmaxf(a, __uint_as_float(s[x][30])), __uint_as_float(s[x][31]));
+          xm = fmaxf(xm, fmaf(fmaxf(a, d), c, bias[x]));
         }
       }
-      auto exceeds = [&](float x) { return x > m + R_TAU || (m == -CUDART_INF_F && x > m); };
-      const float m_old = m;
-      // (the barrier also lets either half overwrite S: both have read theirs)
-      tc_fence_before();
-      if (softmax_any(!ok || exceeds(xm))) {
-        half_sm[h][k_row] = xm;
-        if (softmax_any(!ok)) break;
-        const float x = fmaxf(half_sm[0][k_row], half_sm[1][k_row]);
-        if (exceeds(x)) m = ceilf(x);
+      // the reference that the tile before left
+      if (i > 0 || g > 0) {
+        if (!warp_wait(bar_turn + 16 * quarter + 8 * g, (g ? i : i - 1) & 1, &dead_sm)) break;
+        m = m_sm[k_row];
       }
-      tc_fence_after();
-      const int e_new = packed ? 0 : tile_exponent(i, 1), de = e_new - ev;
+      const float m_old = m;
+      if (xm > m + R_TAU || (m == -CUDART_INF_F && xm > m)) m = ceilf(xm);
+      m_sm[k_row] = m;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_turn + 16 * quarter + 8 * (1 - g));
+      const int e_new = packed ? 0 : batch_exponent(i, 1), de = g == 0 ? e_new - ev : 0;  // (for the second tile O has it already)
       ev = e_new;
-      if (i > 0 && __any_sync(0xffffffffu, m != m_old || de != 0) && !idle) {
-        // O has to follow a raised reference, and the scale of the window's values; each half takes half of the columns
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_o + 8 * ((i - 1) & 1), ((i - 1) >> 1) & 1, &dead_sm));
+      if ((i > 0 || g > 0) && !idle && __any_sync(0xffffffffu, m != m_old || de != 0)) {
+        // O has to follow a raised reference, and the scale of the window's values: after the products of the tile before
+        const int j = g ? i : i - 1;
+        if (!warp_wait(bar_o + 16 * (j & 1) + 8 * (1 - g), (j >> 1) & 1, &dead_sm)) break;
         tc_fence_after();
         const float f = m_old == -CUDART_INF_F ? 0.f : ex2(m_old - m), fv = f * pow2i(de);
 #pragma unroll 1
-        for (int k = h ? D / 2 : 0; k < (h ? Ly::VN : D / 2); k += 16) {
+        for (int k = 0; k < Ly::VN; k += 16) {
           uint32_t y[16];
           tmem_ld<16>(row_t + Ly::COL_O + k, y);
           tc_wait_ld();
@@ -612,30 +635,31 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         // numerators, tokens (0, 2), (1, 3) of four side by side
         const uint64_t cc = pair_of(c, c);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const float off = m == -CUDART_INF_F ? 0.f : bias[g] + ((float)R_PEXP - m);
+        for (int x = 0; x < 2; ++x) {
+          const float off = m == -CUDART_INF_F ? 0.f : bias[x] + ((float)R_PEXP - m);
           const uint64_t oo = pair_of(off, off);
           uint32_t y[16];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[g][4 * k]), __uint_as_float(s[g][4 * k + 1])), cc, oo));
-            const float2 d = halves_of(fma2(pair_of(__uint_as_float(s[g][4 * k + 2]), __uint_as_float(s[g][4 * k + 3])), cc, oo));
+            const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[x][4 * k]), __uint_as_float(s[x][4 * k + 1])), cc, oo));
+            const float2 d = halves_of(fma2(pair_of(__uint_as_float(s[x][4 * k + 2]), __uint_as_float(s[x][4 * k + 3])), cc, oo));
             y[2 * k] = pack_io2<true>(ex2(a.x), ex2(d.x));
             y[2 * k + 1] = pack_io2<true>(ex2(a.y), ex2(d.y));
           }
-          tmem_st<16>(s_t + 32 * h + 16 * g, y);
+          tmem_st<16>(s_t + 16 * x, y);
         }
         tc_wait_st();
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 8 * (i & 1));
+      if (lane == 0) mbar_arrive(bar_p + 16 * b + 8 * g);
     }
 
-    // ---- the result, or the split's partial: each half takes half of the channels ----
+    // ---- the result, or the split's partial: each group takes half of the channels ----
     if (N > 0) mbar_wait(bar_end, 0, &dead_sm);
-    __syncwarp();
+    softmax_sync();  // (every warp comes here, whatever failed)
     tc_fence_after();
+    if (N > 0) m = m_sm[k_row];
     const float unit = pow2i(-R_PEXP), uv = unit * pow2i(-ev);
     float l = 0.f, extra[NG];
     {
@@ -644,39 +668,39 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       tc_wait_ld();
       l = N > 0 ? __uint_as_float(y[8]) * unit : 0.f;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) extra[g] = __uint_as_float(y[g]) + (BV == 2 ? __uint_as_float(y[NG + g]) : 0.f);
+      for (int x = 0; x < NG; ++x) extra[x] = __uint_as_float(y[x]) + (BV == 2 ? __uint_as_float(y[NG + x]) : 0.f);
     }
     const bool empty = N == 0;  // no token: the sums are not defined
     if (!empty && m == -CUDART_INF_F) m = CUDART_NAN_F;  // (no logit is a number, nor is the result)
     const bool store = k_row < n_rows && dead_sm == 0;
     const float inv = p.part_acc != nullptr ? uv : uv / l;
-    const size_t row = store ? call_row(k_row) : 0;
+    const size_t to_row = store ? call_row(k_row) : 0;
 #pragma unroll 1
     for (int k = 0; k < D / 2; k += 16) {
-      const int c0 = h * (D / 2) + k;
+      const int c0 = g * (D / 2) + k;
       uint32_t y[16];
       tmem_ld<16>(row_t + Ly::COL_O + c0, y);
       tc_wait_ld();
       float z = extra[0], v[16];
 #pragma unroll
-      for (int g = 1; g < NG; ++g) z = c0 / GS == g ? extra[g] : z;
+      for (int x = 1; x < NG; ++x) z = c0 / GS == x ? extra[x] : z;
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = empty ? 0.f : (__uint_as_float(y[j]) + z) * inv;
       if (!store) continue;
       if (p.part_acc != nullptr || p.out_f32) {
-        float* const to = (p.part_acc != nullptr ? p.part_acc + (row * p.ns + split) * D : reinterpret_cast<float*>(p.out) + row * D) + c0;
+        float* const to = (p.part_acc != nullptr ? p.part_acc + (to_row * p.ns + split) * D : reinterpret_cast<float*>(p.out) + to_row * D) + c0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) reinterpret_cast<float4*>(to)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
       } else {
         uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = p.f16 ? pack_io2<true>(v[2 * j], v[2 * j + 1]) : pack_io2<false>(v[2 * j], v[2 * j + 1]);
-        uint4* const to = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.out) + row * D + c0);
+        uint4* const to = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.out) + to_row * D + c0);
         to[0] = make_uint4(w[0], w[1], w[2], w[3]);
         to[1] = make_uint4(w[4], w[5], w[6], w[7]);
       }
     }
-    if (store && h == 0 && p.part_acc != nullptr) reinterpret_cast<float2*>(p.part_ml)[row * p.ns + split] = make_float2(m, empty ? 0.f : l);
+    if (store && g == 0 && p.part_acc != nullptr) reinterpret_cast<float2*>(p.part_ml)[to_row * p.ns + split] = make_float2(m, empty ? 0.f : l);
   }
   tc_fence_before();
   __syncthreads();
