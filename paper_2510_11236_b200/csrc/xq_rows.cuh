@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   const uint32_t bar_q = bar_vunit + 8 * R_UNITS;        // Q is written
   const uint32_t bar_end = bar_q + 8;                    // every product is complete
 
-  if (tid == 0) {
+  if (tid == 32 * R_LOAD) {
 #pragma unroll
     for (int i = 0; i < R_RAW; ++i) {
       mbar_init(bar_rfull + 8 * i, 1);
@@ -261,6 +261,41 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     return p.f16 ? 0 : window_exponent(bf16_top(x));
   };
 
+  // a batch's packed data into its raw stage
+  auto load = [&](int i) {
+    const uint32_t dst = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW, bar = bar_rfull + 8 * (i % R_RAW);
+    const size_t t = (size_t)t_lo + i;
+    mbar_expect_tx(bar, Ly::RAW);
+    bulk_load(dst, reinterpret_cast<const uint8_t*>(p.L.k_codes) + (size_t)bh * ((size_t)dm.nq_cap * Ly::KROW) + t * (RB * Ly::KROW), RB * Ly::KROW, bar);
+    bulk_load(dst + Ly::RAW_KM, reinterpret_cast<const uint8_t*>(p.L.k_meta) + (size_t)bh * ((size_t)(dm.nq_cap / GS) * (4 * D)) + t * (RB / GS * 4 * D), RB / GS * 4 * D, bar);
+    bulk_load(dst + Ly::RAW_VC, reinterpret_cast<const uint8_t*>(p.L.v_codes) + (size_t)bh * ((size_t)dm.nq_cap * (D * BV / 8)) + t * (16 * D * BV), 16 * D * BV, bar);
+    bulk_load(dst + Ly::RAW_VM, reinterpret_cast<const uint8_t*>(p.L.v_meta) + (size_t)bh * ((size_t)dm.nq_cap * 4 * NG) + t * (RB * 4 * NG), RB * 4 * NG, bar);
+  };
+  // Before the CTA's first barrier: the first packed batches, and q's rows into the second key operand's place, sixteen rows a
+  // warp, lanes along a row.
+  constexpr int QROW = 2 * D + 16;
+  static_assert(ROWS_TILE * QROW <= Ly::KBYTES, "q fits");
+  const uint32_t q_sm = sm + Ly::KBYTES;
+  if (warp == R_LOAD) {
+    if (lane == 0)
+      for (int i = 0; i < min(R_RAW, n_pk); ++i) load(i);
+    __syncwarp();
+  } else if (warp < 8) {
+    constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES;
+    const int first = 16 * warp;
+    const uint32_t mine = first + (lane & 15) < n_rows ? (uint32_t)call_row(first + (lane & 15)) : 0u;
+    uint4 x[16 / AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < 16 / AT_ONCE; ++k) {
+      const int y = k * AT_ONCE + lane / PIECES;
+      const uint32_t at = __shfl_sync(0xffffffffu, mine, y);
+      x[k] = first + y < n_rows ? reinterpret_cast<const uint4*>(p.q)[(size_t)at * PIECES + lane % PIECES] : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < 16 / AT_ONCE; ++k)
+      sts128(q_sm + (first + k * AT_ONCE + lane / PIECES) * QROW + lane % PIECES * 16, x[k].x, x[k].y, x[k].z, x[k].w);
+  }
+
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -315,22 +350,12 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     }
     __syncwarp();
   } else if (warp == R_LOAD) {
-    // ================= packed data, a batch at a time =================
+    // ================= packed data, a batch at a time (the first ones are on their way) =================
     if (lane == 0) {
-      const size_t first = (size_t)t_lo;
-      const uint8_t* const kc = reinterpret_cast<const uint8_t*>(p.L.k_codes) + (size_t)bh * ((size_t)dm.nq_cap * Ly::KROW) + first * (RB * Ly::KROW);
-      const uint8_t* const vc = reinterpret_cast<const uint8_t*>(p.L.v_codes) + (size_t)bh * ((size_t)dm.nq_cap * (D * BV / 8)) + first * (16 * D * BV);
-      const uint8_t* const km = reinterpret_cast<const uint8_t*>(p.L.k_meta) + (size_t)bh * ((size_t)(dm.nq_cap / GS) * (4 * D)) + first * (RB / GS * 4 * D);
-      const uint8_t* const vm = reinterpret_cast<const uint8_t*>(p.L.v_meta) + (size_t)bh * ((size_t)dm.nq_cap * 4 * NG) + first * (RB * 4 * NG);
-      int i = 0;
+      int i = min(R_RAW, n_pk);
       for (; i < n_pk; ++i) {
-        if (i >= R_RAW && !mbar_wait(bar_rfree + 8 * (i % R_RAW), (i / R_RAW - 1) & 1, &dead_sm)) break;
-        const uint32_t dst = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW, bar = bar_rfull + 8 * (i % R_RAW);
-        mbar_expect_tx(bar, Ly::RAW);
-        bulk_load(dst, kc + (size_t)i * (RB * Ly::KROW), RB * Ly::KROW, bar);
-        bulk_load(dst + Ly::RAW_KM, km + (size_t)i * (RB / GS * 4 * D), RB / GS * 4 * D, bar);
-        bulk_load(dst + Ly::RAW_VC, vc + (size_t)i * (16 * D * BV), 16 * D * BV, bar);
-        bulk_load(dst + Ly::RAW_VM, vm + (size_t)i * (RB * 4 * NG), RB * 4 * NG, bar);
+        if (!mbar_wait(bar_rfree + 8 * (i % R_RAW), (i / R_RAW - 1) & 1, &dead_sm)) break;
+        load(i);
       }
       // no copy may be in flight when the shared memory is released (nobody may have waited for them if a wait gave up)
       for (int k = max(0, i - R_RAW); k < i; ++k)
@@ -376,6 +401,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       const int b = i & 1;
       const bool packed = i < n_pk;
       if (packed && !warp_wait(bar_rfull + 8 * (i % R_RAW), (i / R_RAW) & 1, &dead_sm)) break;
+      if (keys && i == 1 && !warp_wait(bar_q, 0, &dead_sm)) break;  // (q lies there until then)
       if (i >= R_BUFS && !warp_wait((keys ? bar_kfree : bar_vfree) + 8 * b, ((i >> 1) & 1) ^ 1, &dead_sm)) break;
       const uint32_t raw = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW;
       const uint32_t dst = sm + op_off + b * (keys ? Ly::KBYTES : Ly::VBYTES);
@@ -521,11 +547,9 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     {
       // q: half of this thread's row as fp16 in the operands' order, bfloat16 scaled by a power of two into [1, 2), to tensor
       // memory
-      const bool real = k_row < n_rows;
-      const uint4* src = reinterpret_cast<const uint4*>(p.q + (real ? call_row(k_row) * D + g * (D / 2) : 0));
       uint4 x[D / 16];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) x[i] = real ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+      for (int i = 0; i < D / 16; ++i) x[i] = lds128(q_sm + k_row * QROW + g * D + 16 * i);
       float f = 1.f;
       if (!p.f16) {
         uint32_t m = 0u;
@@ -674,7 +698,9 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     if (!empty && m == -CUDART_INF_F) m = CUDART_NAN_F;  // (no logit is a number, nor is the result)
     const bool store = k_row < n_rows && dead_sm == 0;
     const float inv = p.part_acc != nullptr ? uv : uv / l;
-    const size_t to_row = store ? call_row(k_row) : 0;
+    const bool wide = p.part_acc != nullptr || p.out_f32;
+    // through shared memory (the operands' place), so that a row leaves in one piece
+    const uint32_t row_bytes = wide ? 4 * D : 2 * D, mine = sm + k_row * (row_bytes + 16);
 #pragma unroll 1
     for (int k = 0; k < D / 2; k += 16) {
       const int c0 = g * (D / 2) + k;
@@ -686,21 +712,29 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       for (int x = 1; x < NG; ++x) z = c0 / GS == x ? extra[x] : z;
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = empty ? 0.f : (__uint_as_float(y[j]) + z) * inv;
-      if (!store) continue;
-      if (p.part_acc != nullptr || p.out_f32) {
-        float* const to = (p.part_acc != nullptr ? p.part_acc + (to_row * p.ns + split) * D : reinterpret_cast<float*>(p.out) + to_row * D) + c0;
+      if (wide) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) reinterpret_cast<float4*>(to)[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        for (int j = 0; j < 4; ++j)
+          sts128(mine + 4 * c0 + 16 * j, __float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
       } else {
         uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = p.f16 ? pack_io2<true>(v[2 * j], v[2 * j + 1]) : pack_io2<false>(v[2 * j], v[2 * j + 1]);
-        uint4* const to = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.out) + to_row * D + c0);
-        to[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        sts128(mine + 2 * c0, w[0], w[1], w[2], w[3]);
+        sts128(mine + 2 * c0 + 16, w[4], w[5], w[6], w[7]);
       }
     }
-    if (store && g == 0 && p.part_acc != nullptr) reinterpret_cast<float2*>(p.part_ml)[to_row * p.ns + split] = make_float2(m, empty ? 0.f : l);
+    proxy_fence();
+    softmax_sync();
+    if (g == 0 && store) {
+      const size_t to_row = call_row(k_row);
+      uint8_t* const to = p.part_acc != nullptr ? reinterpret_cast<uint8_t*>(p.part_acc + (to_row * p.ns + split) * D)
+                                                : reinterpret_cast<uint8_t*>(p.out) + to_row * row_bytes;
+      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(to), "r"(mine), "r"(row_bytes) : "memory");
+      asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
+      if (p.part_acc != nullptr) reinterpret_cast<float2*>(p.part_ml)[to_row * p.ns + split] = make_float2(m, empty ? 0.f : l);
+      asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
+    }
   }
   tc_fence_before();
   __syncthreads();

@@ -108,13 +108,20 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
 #pragma unroll
     for (int j = 0; j < DPL; ++j) a[j] = none ? a[j] : fmaf(v[j], f, a[j]);
   };
-#pragma unroll 4
-  for (int s = 0; s < p.ns; ++s) {
-    const float2 x = ml[s];
-    float v[DPL];
+  // eight splits' loads at a time: a trip to L2 for each eight
+  for (int s0 = 0; s0 < p.ns; s0 += 8) {
+    float2 x[8];
+    float v[8][DPL];
 #pragma unroll
-    for (int j = 0; j < DPL; j += 2) *reinterpret_cast<float2*>(v + j) = *reinterpret_cast<const float2*>(acc + (size_t)s * D + j);
-    add(x.x, x.y, v);
+    for (int k = 0; k < 8; ++k) {
+      const bool there = s0 + k < p.ns;
+      x[k] = there ? ml[s0 + k] : make_float2(-CUDART_INF_F, 0.f);
+#pragma unroll
+      for (int j = 0; j < DPL; j += 2)
+        *reinterpret_cast<float2*>(&v[k][j]) = there ? *reinterpret_cast<const float2*>(acc + (size_t)(s0 + k) * D + j) : make_float2(0.f, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(x[k].x, x[k].y, v[k]);
   }
   if (p.own != nullptr) {
     float v[DPL];
