@@ -269,8 +269,9 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, const DecodeLay
 // out = sum_s acc_s 2^(m_s-M) / sum_s l_s 2^(m_s-M).  No CTA ever waits for another.
 // What it takes is two trips to L2, one for all (m, l) and one for the partials: a warp that went through its share of
 // the heads one after the other, both trips for each, made it 2.3 us with four heads and 5.1 us with eight.
-// L, part_acc, part_ml: of the first of the CTA's NL layers; weights: NL * G * (ns + 1) floats of shared memory.
-template <int NL>
+// L, part_acc, part_ml: of the first of the CTA's NL layers; weights: NL * G * (ns + 1) floats of shared memory.  RAGGED: a
+// stream may have no token at all, its result is zero.
+template <int NL, bool RAGGED>
 __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const DecodeLayer* L, int ns, int hk, int b,
                                              const float* part_acc, const float* part_ml, unsigned* ticket, int* s_flag,
                                              float* weights) {
@@ -300,7 +301,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       M = x.x;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = lane < ns ? ex2(x.x - M) : 0.f;
+      const float f = lane < ns && !(RAGGED && x.x == -CUDART_INF_F) ? ex2(x.x - M) : 0.f;
       Ls = x.y * f;
       if (lane < ns) w[lane] = f;
     } else {
@@ -309,7 +310,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       for (int s = lane; s < ns; s += 32) {
         const float2 x = ld_cg2(ml + 2 * s);
-        const float f = ex2(x.x - M);
+        const float f = RAGGED && x.x == -CUDART_INF_F ? 0.f : ex2(x.x - M);
         Ls = fmaf(x.y, f, Ls);
         w[s] = f;
       }
@@ -317,7 +318,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
     if (lane == 0) {
-      w[ns] = 1.0f / Ls;
+      w[ns] = RAGGED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
       if (NL == 1 && p.lse != nullptr) p.lse[row_of(v)] = M + log2f(Ls);
     }
   }
@@ -347,7 +348,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
   if (threadIdx.x == 0) *ticket = 0u;  // ready for the next launch on this stream
 }
 
-template <int BK, int BV, int GS, int HP, int NL, bool MANY>
+template <int BK, int BV, int GS, int HP, int NL, bool MANY, bool RAGGED>
 __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Plan<BK, BV, GS, HP, NL, MANY>::CTAS)
     decode_mma_kernel(const __grid_constant__ DecodeParams p) {
   using Pl = Plan<BK, BV, GS, HP, NL, MANY>;
@@ -400,15 +401,24 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     const unsigned stream = blockIdx.x / (unsigned)p.ns_q;
     const int split = (int)(blockIdx.x - stream * (unsigned)p.ns_q);
     const int bh = (int)stream, b = (int)(stream / (unsigned)dm.Hkv);
-    const int nbt = (p.n_q + BT - 1) / BT;  // batches of the stream (the last one may be ragged)
+    int n_q = p.n_q, r = p.r;
+    if constexpr (RAGGED) {
+      // the tokens of this sequence that exist; lengths may come from the preceding kernel
+      if (!p.late_wait) grid_dependency_wait();
+      const int S = max(0, min(n_q + r, p.lengths[b]));
+      n_q = min(n_q, S);
+      r = S - n_q;
+      place_sm[7] = n_q;
+    }
+    const int nbt = (n_q + BT - 1) / BT;  // batches of the stream (the last one may be ragged)
     // the larger shares come last, with the run that may be short
     const int runs = p.deal == 1 ? nbt : (nbt + p.deal - 1) / p.deal;
     int lo, hi, wt0, wt1;
     share_of(runs, p.ns_q, p.ns_q - 1 - split, lo, hi);
     const int b0 = (runs - hi) * p.deal, b1 = min((runs - lo) * p.deal, nbt);
-    share_of(p.r, p.ns_q, split, wt0, wt1);
+    share_of(r, p.ns_q, split, wt0, wt1);
     // half batches (the last half of the stream's last batch may be empty)
-    const int halves = b1 > b0 ? 2 * (b1 - b0) - (b1 == nbt && nbt * BT - p.n_q >= TT ? 1 : 0) : 0;
+    const int halves = b1 > b0 ? 2 * (b1 - b0) - (b1 == nbt && nbt * BT - n_q >= TT ? 1 : 0) : 0;
     place_sm[0] = b0; place_sm[1] = halves; place_sm[2] = wt0; place_sm[3] = wt1;
     place_sm[4] = b; place_sm[5] = bh - b * dm.Hkv; place_sm[6] = split;
     dead_sm = 0;
@@ -644,7 +654,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
   int last_k = 0, last_v = 0;  // rounds whose key codes, values were copied last
 #pragma unroll 1
   for (int r = 0; r < rounds; ++r) {
-    const int valid = min(TT, p.n_q - b0 * BT - (warp + W * r) * TT);  // < TT only in the stream's last round
+    const int valid = min(TT, (RAGGED ? place2.w : p.n_q) - b0 * BT - (warp + W * r) * TT);  // < TT only in the stream's last round
     if (!__all_sync(0xffffffffu, mbar_wait(bar_k, r & 1, &dead_sm))) break;
 
     if (valid < TT) {  // what no token has reached may be anything: no scale, no zero-point
@@ -1310,6 +1320,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     for (int t = wrow0; t < wrow1; ++t) add(row((t + halves) % W, true));
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
+      if (RAGGED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
       store_out(p, LL[layer], hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
       if (NL == 1 && d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
     } else {
@@ -1319,14 +1330,14 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     }
   }
   if (ns > 1)
-    ticket_merge<NL>(p, LL, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
+    ticket_merge<NL, RAGGED>(p, LL, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
                         reinterpret_cast<float*>(smem));
 }
 
 template <int BK, int BV, int GS, int HP, int NL, bool MANY>
 cudaError_t launch_one(const DecodeParams& p, cudaStream_t st) {
   using Pl = Plan<BK, BV, GS, HP, NL, MANY>;
-  return launch_dependent(decode_mma_kernel<BK, BV, GS, HP, NL, MANY>, dim3((unsigned)(p.ns_q * p.dm.B * p.dm.Hkv), p.n_layers / NL), dim3(Pl::WARPS * 32),
+  return launch_dependent(decode_mma_kernel<BK, BV, GS, HP, NL, MANY, false>, dim3((unsigned)(p.ns_q * p.dm.B * p.dm.Hkv), p.n_layers / NL), dim3(Pl::WARPS * 32),
                           (size_t)Pl::TOTAL, st, p);
 }
 
@@ -1334,12 +1345,23 @@ cudaError_t launch_one(const DecodeParams& p, cudaStream_t st) {
 template <int BK, int BV, int GS, int HP, int NL, bool MANY>
 MmaShape shape_one() {
   using Pl = Plan<BK, BV, GS, HP, NL, MANY>;
-  auto kernel = decode_mma_kernel<BK, BV, GS, HP, NL, MANY>;
+  auto kernel = decode_mma_kernel<BK, BV, GS, HP, NL, MANY, false>;
   // the largest shared-memory carve-out: two or three CTAs of this size are to share an SM
   const bool ready = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Pl::TOTAL) == cudaSuccess &&
                      cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100) == cudaSuccess;
   if (!ready) cudaGetLastError();
   return {Pl::WARPS, ready};
+}
+
+// The variant for sequences of their own lengths: its launches are fewer, and it is prepared with each.
+template <int BK, int BV, int GS, int HP, int NL, bool MANY>
+cudaError_t launch_ragged_one(const DecodeParams& p, cudaStream_t st) {
+  using Pl = Plan<BK, BV, GS, HP, NL, MANY>;
+  auto kernel = decode_mma_kernel<BK, BV, GS, HP, NL, MANY, true>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Pl::TOTAL);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3((unsigned)(p.ns_q * p.dm.B * p.dm.Hkv), 1), dim3(Pl::WARPS * 32), (size_t)Pl::TOTAL, st, p);
 }
 
 #define XQ_DISPATCH(FN, ...)                               \
@@ -1360,6 +1382,14 @@ template <int HP, int NL, bool MANY>
 cudaError_t launch_decode_mma_t(const DecodeParams& p, cudaStream_t st) {
   const int bk = p.layer[0].L.bk, bv = p.layer[0].L.bv, g = p.dm.g;
   XQ_DISPATCH(launch_one, p, st)
+  return cudaErrorInvalidValue;
+}
+template <int HP>
+cudaError_t launch_decode_ragged_t(const DecodeParams& p, cudaStream_t st) {
+  constexpr int NL = 1;
+  constexpr bool MANY = false;
+  const int bk = p.layer[0].L.bk, bv = p.layer[0].L.bv, g = p.dm.g;
+  XQ_DISPATCH(launch_ragged_one, p, st)
   return cudaErrorInvalidValue;
 }
 template <int HP, int NL, bool MANY>

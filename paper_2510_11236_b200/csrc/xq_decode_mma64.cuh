@@ -223,7 +223,8 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, const DecodeLay
 // out = sum_s acc_s 2^(m_s-M) / sum_s l_s 2^(m_s-M).  No CTA ever waits for another.
 // What it takes is two trips to L2, one for all (m, l) and one for the partials: a warp that went through its share of
 // the heads one after the other, both trips for each, made it 2.3 us with four heads and 5.1 us with eight.
-// weights: G * (ns + 1) floats of shared memory.
+// weights: G * (ns + 1) floats of shared memory.  RAGGED: a stream may have no token at all, its result is zero.
+template <bool RAGGED>
 __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const DecodeLayer& L, int ns, int hk, int b,
                                              const float* part_acc, const float* part_ml, unsigned* ticket, int* s_flag,
                                              float* weights) {
@@ -252,7 +253,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       M = x.x;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = lane < ns ? ex2(x.x - M) : 0.f;
+      const float f = lane < ns && !(RAGGED && x.x == -CUDART_INF_F) ? ex2(x.x - M) : 0.f;
       Ls = x.y * f;
       if (lane < ns) w[lane] = f;
     } else {
@@ -261,7 +262,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       for (int s = lane; s < ns; s += 32) {
         const float2 x = ld_cg2(ml + 2 * s);
-        const float f = ex2(x.x - M);
+        const float f = RAGGED && x.x == -CUDART_INF_F ? 0.f : ex2(x.x - M);
         Ls = fmaf(x.y, f, Ls);
         w[s] = f;
       }
@@ -269,7 +270,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
     if (lane == 0) {
-      w[ns] = 1.0f / Ls;
+      w[ns] = RAGGED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
       if (p.lse != nullptr) p.lse[hq0 + h] = M + log2f(Ls);
     }
   }
@@ -298,7 +299,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
   if (threadIdx.x == 0) *ticket = 0u;  // ready for the next launch on this stream
 }
 
-template <int BK, int BV, int GS, int HP, int NT>
+template <int BK, int BV, int GS, int HP, int NT, bool RAGGED>
 __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK, BV, GS, HP, NT>::CTAS)
     decode_mma64_kernel(const __grid_constant__ DecodeParams p) {
   using Pl = Plan<BK, BV, GS, HP, NT>;
@@ -329,7 +330,15 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
   const int split = (int)(blockIdx.x - stream * (unsigned)ns);
   const int hk = (int)(stream % (unsigned)dm.Hkv), b = (int)(stream / (unsigned)dm.Hkv);
   const int bh = b * dm.Hkv + hk;
-  const int nbt = (p.n_q + BT - 1) / BT;  // batches of the stream (the last one may be ragged)
+  int n_q = p.n_q, r = p.r;
+  if constexpr (RAGGED) {
+    // the tokens of this sequence that exist; lengths may come from the preceding kernel
+    if (!p.late_wait) grid_dependency_wait();
+    const int S = max(0, min(n_q + r, p.lengths[b]));
+    n_q = min(n_q, S);
+    r = S - n_q;
+  }
+  const int nbt = (n_q + BT - 1) / BT;  // batches of the stream (the last one may be ragged)
   int b0, b1, wt0, wt1;
   {
     // the larger shares come last, with the run that may be short
@@ -339,7 +348,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
     b0 = (runs - hi) * p.deal;
     b1 = min((runs - lo) * p.deal, nbt);
   }
-  share_of(p.r, ns, split, wt0, wt1);
+  share_of(r, ns, split, wt0, wt1);
   const int nb = b1 - b0;
 
   const uint32_t sm_base = (uint32_t)__cvta_generic_to_shared(smem);
@@ -489,7 +498,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
   int last_k = 0, last_v = 0;  // number of the copy that each barrier was armed for last
 #pragma unroll 1
   for (int i = warp, it = 0; i < nb; i += W, ++it) {
-    const int valid = min(BT, p.n_q - (b0 + i) * BT);  // < BT only in the stream's last batch
+    const int valid = min(BT, (RAGGED ? n_q : p.n_q) - (b0 + i) * BT);  // < BT only in the stream's last batch
     if (!__all_sync(0xffffffffu, mbar_wait(bar_k, it & 1, &dead_sm))) break;
 
     // ---- keys: scales into the order of the operand slots (in place), the largest of them ----
@@ -988,6 +997,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
     }
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
+      if (RAGGED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
       store_out(p, L, hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
       if (d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
     } else {
@@ -996,14 +1006,14 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
     }
   }
   if (ns > 1)
-    ticket_merge(p, L, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
+    ticket_merge<RAGGED>(p, L, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
                     reinterpret_cast<float*>(smem));
 }
 
 template <int BK, int BV, int GS, int HP, int NT>
 cudaError_t launch_one(const DecodeParams& p, cudaStream_t st) {
   using Pl = Plan<BK, BV, GS, HP, NT>;
-  return launch_dependent(decode_mma64_kernel<BK, BV, GS, HP, NT>, dim3((unsigned)(p.ns_q * p.dm.B * p.dm.Hkv), p.n_layers), dim3(Pl::WARPS * 32),
+  return launch_dependent(decode_mma64_kernel<BK, BV, GS, HP, NT, false>, dim3((unsigned)(p.ns_q * p.dm.B * p.dm.Hkv), p.n_layers), dim3(Pl::WARPS * 32),
                           (size_t)Pl::TOTAL, st, p);
 }
 
@@ -1011,12 +1021,23 @@ cudaError_t launch_one(const DecodeParams& p, cudaStream_t st) {
 template <int BK, int BV, int GS, int HP, int NT>
 MmaShape shape_one() {
   using Pl = Plan<BK, BV, GS, HP, NT>;
-  auto kernel = decode_mma64_kernel<BK, BV, GS, HP, NT>;
+  auto kernel = decode_mma64_kernel<BK, BV, GS, HP, NT, false>;
   // the largest shared-memory carve-out: two CTAs of this size are to share an SM
   const bool ready = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Pl::TOTAL) == cudaSuccess &&
                      cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100) == cudaSuccess;
   if (!ready) cudaGetLastError();
   return {Pl::WARPS, ready};
+}
+
+// The variant for sequences of their own lengths: its launches are fewer, and it is prepared with each.
+template <int BK, int BV, int GS, int HP, int NT>
+cudaError_t launch_ragged_one(const DecodeParams& p, cudaStream_t st) {
+  using Pl = Plan<BK, BV, GS, HP, NT>;
+  auto kernel = decode_mma64_kernel<BK, BV, GS, HP, NT, true>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Pl::TOTAL);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, dim3((unsigned)(p.ns_q * p.dm.B * p.dm.Hkv), 1), dim3(Pl::WARPS * 32), (size_t)Pl::TOTAL, st, p);
 }
 
 #define XQ_DISPATCH(FN, ...)                               \
@@ -1037,6 +1058,12 @@ template <int HP, int NT>
 cudaError_t launch_decode_mma64_t(const DecodeParams& p, cudaStream_t st) {
   const int bk = p.layer[0].L.bk, bv = p.layer[0].L.bv, g = p.dm.g;
   XQ_DISPATCH(launch_one, p, st)
+  return cudaErrorInvalidValue;
+}
+template <int HP, int NT>
+cudaError_t launch_decode_ragged64_t(const DecodeParams& p, cudaStream_t st) {
+  const int bk = p.layer[0].L.bk, bv = p.layer[0].L.bv, g = p.dm.g;
+  XQ_DISPATCH(launch_ragged_one, p, st)
   return cudaErrorInvalidValue;
 }
 template <int HP, int NT>

@@ -120,10 +120,10 @@ void make_plan(const xq_config* c, Plan& pl) {
   pl.total = off;
 }
 
-// Rows calls (prefix and cross attention): CTAs that splits make, at most, in waves of the device; what a CTA's start and end
-// and a partial of a row cost, in tiles of 64 tokens.
+// Rows calls (prefix and cross attention): CTAs that splits make, at most, in waves of the device; and times, us: of a CTA's
+// batch, of its start and end, of a join, of a row's partial.
 constexpr int ROWS_WAVES = 4;
-constexpr double ROWS_FIXED = 8.0, ROWS_JOIN = 1e-4;
+constexpr double ROWS_BATCH = 1.35, ROWS_FIXED = 9.5, ROWS_JOIN = 2.0, ROWS_PART = 2e-4;
 
 constexpr int N_KINDS = 4;
 constexpr int TIMING_POOL = 1 << 15;
@@ -223,6 +223,7 @@ bool uses_mma(const xq_cache* c) {
 #define XQ_MMA128(FN, ...) (dm.G == 1 ? FN<1, 1, false>(__VA_ARGS__) : dm.G == 2 ? FN<2, 1, false>(__VA_ARGS__) : dm.G <= 4 ? FN<4, 1, false>(__VA_ARGS__) : FN<8, 1, false>(__VA_ARGS__))
 #define XQ_MMA_MANY(FN, ...) (dm.G == 1 ? FN<1, 1, true>(__VA_ARGS__) : dm.G == 2 ? FN<2, 1, true>(__VA_ARGS__) : FN<4, 1, true>(__VA_ARGS__))
 #define XQ_MMA_PAIRS(FN, ...) (dm.G == 1 ? FN<1, 2, false>(__VA_ARGS__) : dm.G == 2 ? FN<2, 2, false>(__VA_ARGS__) : FN<4, 2, false>(__VA_ARGS__))
+#define XQ_MMA_RAGGED(FN, ...) (dm.G == 1 ? FN<1>(__VA_ARGS__) : dm.G == 2 ? FN<2>(__VA_ARGS__) : dm.G <= 4 ? FN<4>(__VA_ARGS__) : FN<8>(__VA_ARGS__))
 #define XQ_MMA64(FN, ...) (dm.G == 1 ? FN<1, 1>(__VA_ARGS__) : dm.G == 2 ? FN<2, 1>(__VA_ARGS__) : dm.G <= 4 ? FN<4, 1>(__VA_ARGS__) : FN<4, 2>(__VA_ARGS__))
 
 cudaError_t launch_decode_mma(const DecodeParams& p, cudaStream_t st) {
@@ -230,6 +231,7 @@ cudaError_t launch_decode_mma(const DecodeParams& p, cudaStream_t st) {
   if (p.paired && p.n_layers % 2) return cudaErrorInvalidValue;  // (the last one would have no CTA)
   if (p.paired) return XQ_MMA_PAIRS(launch_decode_mma_t, p, st);
   if (p.many) return XQ_MMA_MANY(launch_decode_mma_t, p, st);
+  if (p.lengths) return dm.D == 128 ? XQ_MMA_RAGGED(launch_decode_ragged_t, p, st) : XQ_MMA64(launch_decode_ragged64_t, p, st);
   return dm.D == 128 ? XQ_MMA128(launch_decode_mma_t, p, st) : XQ_MMA64(launch_decode_mma64_t, p, st);
 }
 
@@ -495,6 +497,7 @@ int prepare_decode(const xq_cache* c, int layer, const void* q, void* out, int o
   p.late_wait = 0;
   p.f16 = c->cfg.io_dtype == XQ_F16;
   p.lse = nullptr;
+  p.lengths = nullptr;
   return XQ_OK;
 }
 
@@ -1031,20 +1034,18 @@ RowsPlan rows_plan(const xq_cache* kv, int Bq, int T) {
   return r;
 }
 
-// Splits of a call: modelled times in units of a 64-token tile.  A launch's CTAs go in waves; a CTA costs its tiles and
-// ROWS_FIXED more, and a partial that is written and read again costs each row something.
+// Modelled time of a call, us: a launch's CTAs go in waves; a CTA costs its batches of 128 tokens and its start and end, and
+// partials are written and read again.
+double rows_time(const xq_cache* kv, const RowsPlan& r, int S, int ns) {
+  const int batches = (S + 127) / 128;
+  const double waves = ceil((double)(r.ctas * ns) / kv->sm_count);
+  return waves * (ROWS_BATCH * ((batches + ns - 1) / ns) + ROWS_FIXED) + (ns > 1 ? ROWS_JOIN + ROWS_PART * (double)r.rows * ns : 0.0);
+}
 int rows_splits(const xq_cache* kv, const RowsPlan& r, int S) {
-  const int batches = (S + 127) / 128, most = std::min(rows_most_splits(kv, r.ctas), std::max(1, batches));
+  const int most = std::min(rows_most_splits(kv, r.ctas), std::max(1, (S + 127) / 128));
   int best = 1;
-  double best_time = 0.0;
-  for (int ns = 1; ns <= most; ++ns) {
-    const double waves = ceil((double)(r.ctas * ns) / kv->sm_count), tiles = 2.0 * ((batches + ns - 1) / ns);
-    const double time = waves * (tiles + ROWS_FIXED) + (ns > 1 ? ROWS_JOIN * (double)r.rows * ns : 0.0);
-    if (ns == 1 || time < best_time) {
-      best = ns;
-      best_time = time;
-    }
-  }
+  for (int ns = 2; ns <= most; ++ns)
+    if (rows_time(kv, r, S, ns) < rows_time(kv, r, S, best)) best = ns;
   return best;
 }
 
@@ -1103,7 +1104,7 @@ int launch_rows(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, i
   return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
 }
 
-int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_acc, const float* part_ml, const float* own,
+int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_acc, const float* part_ml, const float* part_lse, const float* own,
                      const float* own_lse, void* out, int out_f32, cudaStream_t st) {
   JoinParams p;
   p.rows = r.rows;
@@ -1111,6 +1112,7 @@ int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_a
   p.ns = ns;
   p.part_acc = part_acc;
   p.part_ml = part_ml;
+  p.part_lse = part_lse;
   p.own = own;
   p.own_lse = own_lse;
   p.out = out;
@@ -1123,6 +1125,43 @@ int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_a
   }
   c->launches++;
   return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
+}
+
+// Query tokens of each sequence against a whole cache in decode launches, one for each of the T tokens, chained (where the rows
+// of a kv head are few: see rows_one_by_one).  kv: the cache that is read; c: the handle whose scratch and status word the call
+// uses.  lse: [T,B,Hq] or null.
+int launch_rows_decode(xq_cache* c, xq_cache* kv, int layer, int T, const int* lengths, const void* q, void* out, int out_f32,
+                       float* lse, cudaStream_t st) {
+  const Dims& dm = kv->plan.dm;
+  const size_t rows = (size_t)dm.B * dm.Hq;
+  for (int j = 0; j < T; ++j) {
+    DecodeParams p;
+    bool use_mma = false;
+    int rc = prepare_decode(kv, layer, (const uint8_t*)q + j * rows * dm.D * 2, (uint8_t*)out + j * rows * dm.D * (out_f32 ? 4 : 2), out_f32,
+                            nullptr, nullptr, kv->seq[layer], p, use_mma);
+    if (rc != XQ_OK) return rc;
+    p.scale = c->scale;
+    p.lse = lse ? lse + j * rows : nullptr;
+    p.lengths = lengths;
+    if (j > 0) p.early_fetch = p.late_wait = 1;  // what this launch reads was complete when the first one had waited
+    rc = launch_decode(c, p, use_mma, workspace_scratch(c), st);
+    if (rc != XQ_OK) {
+      c->tickets_clean = false;
+      return rc;
+    }
+  }
+  return XQ_OK;
+}
+
+// Whether T query tokens of each sequence take less time as decode launches than as one rows call (one sequence of queries for
+// each of the cache, heads that the tensor-core decode kernels take).  Modelled times in us: decode as plan_batches has them;
+// rows as rows_splits does.
+bool rows_one_by_one(const xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, int T, int ns) {
+  const Dims& dm = kv->plan.dm;
+  if (r.each != 1 || T > 16 || !uses_mma(kv) || c->cfg.kernel == XQ_KERNEL_GENERIC) return false;
+  const int S = kv->seq[layer], batches = (S - residual_count(S, dm.R) + XQ_BATCH - 1) / XQ_BATCH;
+  const MmaPlan window{0, 0, 1, decode_times(dm).launch, 2.5}, &plan = batches > 0 ? batches_plan(kv, layer, batches) : window;
+  return plan.alone + (T - 1) * plan.next < rows_time(kv, r, S, ns);
 }
 
 // Whether the handle's device is the current one (a handle made without a device has none).
@@ -1171,11 +1210,17 @@ int prefix_impl(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* o
     rc = chunk_impl(c, layer, q, own, T, 1, stream, lse);
     if (rc != XQ_OK) return rc;
   }
+  if (rows_one_by_one(c, prefix, layer, plan, T, ns)) {
+    if (S == 0) return launch_rows_decode(c, prefix, layer, T, nullptr, q, out, out_f32, nullptr, st);
+    rc = launch_rows_decode(c, prefix, layer, T, nullptr, q, acc, 1, ml, st);
+    if (rc != XQ_OK) return rc;
+    return launch_rows_join(c, plan, 1, acc, nullptr, ml, own, lse, out, out_f32, st);
+  }
   // (one split of the prefix alone: the kernel writes the result)
   const bool direct = ns == 1 && S == 0 && c->cfg.kernel != XQ_KERNEL_GENERIC;
   rc = launch_rows(c, prefix, layer, plan, T, ns, nullptr, q, out, out_f32, direct ? nullptr : acc, ml, st);
   if (rc != XQ_OK || direct) return rc;
-  return launch_rows_join(c, plan, ns, acc, ml, own, lse, out, out_f32, st);
+  return launch_rows_join(c, plan, ns, acc, ml, nullptr, own, lse, out, out_f32, st);
 }
 
 int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const int32_t* lengths, int out_f32, void* workspace,
@@ -1199,10 +1244,11 @@ int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const in
   if (rc != XQ_OK) return rc;
   uint8_t* w = (uint8_t*)workspace;
   float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml);
+  if (rows_one_by_one(c, c, layer, plan, T, ns)) return launch_rows_decode(c, c, layer, T, lengths, q, out, out_f32, nullptr, st);
   const bool direct = ns == 1 && c->cfg.kernel != XQ_KERNEL_GENERIC;
   rc = launch_rows(c, c, layer, plan, T, ns, lengths, q, out, out_f32, direct ? nullptr : acc, ml, st);
   if (rc != XQ_OK || direct) return rc;
-  return launch_rows_join(c, plan, ns, acc, ml, nullptr, nullptr, out, out_f32, st);
+  return launch_rows_join(c, plan, ns, acc, ml, nullptr, nullptr, nullptr, out, out_f32, st);
 }
 
 // Whether a cache of `src`'s data can be held by `dst`: everything that decides what the bytes of a sequence mean.

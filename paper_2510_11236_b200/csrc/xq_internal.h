@@ -115,6 +115,7 @@ struct DecodeParams {
   // [B,Hq] or null (launches of one layer): log2 of each result's softmax denominator, sum 2^(logit / ln 2), for callers
   // that join the result with another one over other tokens
   float* lse;
+  const int* lengths;  // [B] or null: the tokens of each sequence that exist (the variants of the tensor-core kernels for it)
   DecodeLayer layer[DECODE_MAX_LAYERS];
 };
 
@@ -181,6 +182,7 @@ struct JoinParams {
   int D, ns;
   const float* part_acc;
   const float* part_ml;
+  const float* part_lse; // [rows] or null: there is one partial, a result with this denominator (as in DecodeParams)
   const float* own;      // [rows,D] or null
   const float* own_lse;  // [rows]
   void* out;
@@ -255,6 +257,11 @@ template <int HP, int NT>
 cudaError_t launch_decode_mma64_t(const DecodeParams& p, cudaStream_t st);
 template <int HP, int NT>
 MmaShape decode_mma64_shape_t(int g, int bk, int bv);
+// the same, of one layer, for sequences of their own lengths
+template <int HP>
+cudaError_t launch_decode_ragged_t(const DecodeParams& p, cudaStream_t st);
+template <int HP, int NT>
+cudaError_t launch_decode_ragged64_t(const DecodeParams& p, cudaStream_t st);
 template <int D>
 cudaError_t launch_chunk_t(const ChunkParams& p, cudaStream_t st);
 cudaError_t launch_merge(const MergeParams& p, cudaStream_t st);

@@ -95,7 +95,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
   const float* acc = p.part_acc + row * p.ns * D + lane * DPL;
   const float lse = p.own != nullptr ? p.own_lse[row] : -CUDART_INF_F;
   float M = lse;
-  for (int s = lane; s < p.ns; s += 32) M = fmaxf(M, ml[s].x);
+  auto state = [&](int s) { return p.part_lse != nullptr ? make_float2(p.part_lse[row], 1.f) : ml[s]; };
+  for (int s = lane; s < p.ns; s += 32) M = fmaxf(M, state(s).x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   float a[DPL], L = 0.f;
@@ -115,7 +116,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const bool there = s0 + k < p.ns;
-      x[k] = there ? ml[s0 + k] : make_float2(-CUDART_INF_F, 0.f);
+      x[k] = there ? state(s0 + k) : make_float2(-CUDART_INF_F, 0.f);
 #pragma unroll
       for (int j = 0; j < DPL; j += 2)
         *reinterpret_cast<float2*>(&v[k][j]) = there ? *reinterpret_cast<const float2*>(acc + (size_t)(s0 + k) * D + j) : make_float2(0.f, 0.f);

@@ -261,6 +261,14 @@ def test_prefix_several_tokens(shape, kernel, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[3], SHAPES[7]])
+@pytest.mark.parametrize("S,T", [(40, 1), (0, 1), (7, 3)])
+def test_prefix_of_its_own(shape, S, T):
+    # a prompt for every sequence: as many caches as sequences
+    _prefix_case(shape, xq.XQ_KERNEL_AUTO, 3, 1, 333, S, T)
+
+
+@pytest.mark.gpu
 def test_prefix_more_rows_than_a_tile():
     # 3 sequences x 20 tokens x 4 heads = 240 rows; 23 x 12 = 276
     _prefix_case(SHAPES[0], xq.XQ_KERNEL_AUTO, 1, 3, 300, 20, 20)
@@ -299,30 +307,34 @@ def _cross_case(shape, kernel, B, S, T, lengths=None, seed=0, fill=None):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("T", [3, 17])  # few tokens go to the decode kernels, one by one
 @pytest.mark.parametrize("shape", SHAPES)
-def test_cross_shapes(shape, kernel):
-    _cross_case(shape, kernel, 3, 275, 3, lengths=[275, 100, 17])
+def test_cross_shapes(shape, T, kernel):
+    _cross_case(shape, kernel, 3, 275, T, lengths=[275, 100, 17])
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("T", [1, 18])
 @pytest.mark.parametrize("S", [1, 2, 63, 64, 65, 128, 129, 191, 193, 257, 700])
-def test_cross_all_tokens(kernel, S):
-    _cross_case(SHAPES[0], kernel, 2, S, 1, seed=S)
+def test_cross_all_tokens(kernel, S, T):
+    _cross_case(SHAPES[0], kernel, 2, S, T, seed=S)
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kernel", KERNELS)
 @pytest.mark.parametrize("lengths", [[0, 0, 0, 0], [0, 1, 400, 399], [31, 32, 33, 63], [64, 65, 127, 128], [-5, 401, 2 ** 31 - 1, -2 ** 31],
                                      [384, 385, 383, 200]])
-def test_cross_lengths(kernel, lengths):
-    _cross_case(SHAPES[0], kernel, 4, 400, 2, lengths=lengths)
+@pytest.mark.parametrize("shape,T", [(SHAPES[0], 2), (SHAPES[0], 17), (SHAPES[6], 1), (SHAPES[1], 1)])
+def test_cross_lengths(kernel, lengths, shape, T):
+    _cross_case(shape, kernel, 4, 400, T, lengths=lengths)
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kernel", KERNELS)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_cross_masked_tokens_that_are_not_finite(kernel, bad):
+@pytest.mark.parametrize("T", [2, 17])
+def test_cross_masked_tokens_that_are_not_finite(kernel, bad, T):
     # what lies behind a sequence's length reaches nothing: window rows and the packed tokens' parameters
     shape, S = SHAPES[0], 300
 
@@ -336,7 +348,7 @@ def test_cross_masked_tokens_that_are_not_finite(kernel, bad):
             v[2, :, 70:] = h - 65536 if h >= 32768 else h
             k = cache.region(layer, 2).view(torch.int16).view(3, 2, -1, 256)
             k[2, :, 3:] = h - 65536 if h >= 32768 else h  # token groups from 96 on
-    _cross_case(shape, kernel, 3, S, 2, lengths=[300, 256, 70], fill=fill)
+    _cross_case(shape, kernel, 3, S, T, lengths=[300, 256, 70], fill=fill)
 
 
 @pytest.mark.gpu
