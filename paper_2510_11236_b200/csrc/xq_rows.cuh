@@ -227,16 +227,22 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     dead_sm = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
-  // (tensor memory is asked for after the wait: a CTA of the preceding kernel that shares the SM may still have to get its own)
-  grid_dependency_wait();
-  grid_dependents_go();
-  if (warp == R_MMA) tmem_alloc((uint32_t)__cvta_generic_to_shared(&tmem_base_sm), 512u);
-
   // ---- the CTA's rows and batches ----
   const int G = dm.G;
   const int split = blockIdx.x % p.ns, rest = blockIdx.x / p.ns, rt = rest % p.row_tiles, bh = rest / p.row_tiles;
   const int u = bh / dm.Hkv, hk = bh - u * dm.Hkv;
   const int row0 = rt * ROWS_TILE, n_rows = min(ROWS_TILE, p.T * p.each * G - row0);
+  auto call_row = [&](int k) {  // of the stream's row row0 + k
+    const int x = row0 + k, h = x % G, ji = x / G, i = ji % p.each, j = ji / p.each;
+    return ((size_t)j * (dm.B * p.each) + (size_t)u * p.each + i) * dm.Hq + hk * G + h;
+  };
+  const int my_row = 16 * warp + (lane & 15);  // of q, for the warps that fetch it
+  const uint32_t my_call_row = warp < 8 && my_row < n_rows ? (uint32_t)call_row(my_row) : 0u;
+
+  // (tensor memory is asked for after the wait: a CTA of the preceding kernel that shares the SM may still have to get its own)
+  grid_dependency_wait();
+  grid_dependents_go();
+  if (warp == R_MMA) tmem_alloc((uint32_t)__cvta_generic_to_shared(&tmem_base_sm), 512u);
   int n_q = p.n_q, r = p.r;
   if (p.lengths != nullptr) {
     const int S = max(0, min(n_q + r, p.lengths[u]));
@@ -248,10 +254,6 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   share_of(all_batches, p.ns, split, t_lo, t_hi);
   const int N = t_hi - t_lo;
   const int n_pk = max(0, min(t_hi, pk_batches) - t_lo);  // packed batches of the range; batch i is window batch i - n_pk
-  auto call_row = [&](int k) {                            // of the stream's row row0 + k
-    const int x = row0 + k, h = x % G, ji = x / G, i = ji % p.each, j = ji / p.each;
-    return ((size_t)j * (dm.B * p.each) + (size_t)u * p.each + i) * dm.Hq + hk * G + h;
-  };
   // exponent of a window batch's keys (0) or values (1)
   auto batch_exponent = [&](int i, int which) {
     const uint32_t* m = unit_sm[(i - n_pk) % R_UNITS][which];
@@ -283,12 +285,11 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   } else if (warp < 8) {
     constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES;
     const int first = 16 * warp;
-    const uint32_t mine = first + (lane & 15) < n_rows ? (uint32_t)call_row(first + (lane & 15)) : 0u;
     uint4 x[16 / AT_ONCE];
 #pragma unroll
     for (int k = 0; k < 16 / AT_ONCE; ++k) {
       const int y = k * AT_ONCE + lane / PIECES;
-      const uint32_t at = __shfl_sync(0xffffffffu, mine, y);
+      const uint32_t at = __shfl_sync(0xffffffffu, my_call_row, y);
       x[k] = first + y < n_rows ? reinterpret_cast<const uint4*>(p.q)[(size_t)at * PIECES + lane % PIECES] : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
@@ -733,7 +734,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(to), "r"(mine), "r"(row_bytes) : "memory");
       asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
       if (p.part_acc != nullptr) reinterpret_cast<float2*>(p.part_ml)[to_row * p.ns + split] = make_float2(m, empty ? 0.f : l);
-      asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
+      asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
     }
   }
   tc_fence_before();
