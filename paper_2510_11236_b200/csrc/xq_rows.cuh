@@ -15,12 +15,12 @@
 // codes and numerators, as the chunk kernel has them, that is 608 in place of 1280 cycles of the tensor pipe a tile, and half
 // the expansion.
 //
-// Tokens go in batches of 128, two tiles each.  Two groups of four softmax warps (thread = row = lane of tensor memory) take
-// the first and the second tiles; with two S the products run a batch ahead, and one group can compute exponentials while the
-// other reads and searches its S.  The softmax reference of a row is passed from one group to the other in the order of the
-// tiles, before the exponentials, and is raised only when a logit exceeds it by R_TAU (log2 units), which takes a pass over O.
-// P takes columns of its S.  Eight warps expand (four keys, four values), one issues products, one copies packed data.  Window
-// tokens go into the same operands as they are, bfloat16 ones scaled by a power of two for each batch.
+// Tokens go in batches of 128, two tiles each, with two S.  Four groups of four softmax warps (thread = row = lane of tensor
+// memory) take the tiles in turn: a warp's steps are short and wait for one another, so it takes several to fill the SM.  The
+// softmax reference of a row is passed from group to group in the order of the tiles, before the exponentials, and is raised
+// only when a logit exceeds it by R_TAU (log2 units), which takes a pass over O.  P takes columns of its S.  Eight warps expand
+// (four keys, four values), one issues products, one copies packed data.  Window tokens go into the same operands as they are,
+// bfloat16 ones scaled by a power of two for each batch.
 //
 // Every wait on an mbarrier is bounded, as in the chunk kernel: a thread that gives up sets a flag that ends the others' waits,
 // and the CTA reports through the status word.
@@ -38,8 +38,9 @@ constexpr int R_BUFS = 2;        // expanded batches of keys, of values
 constexpr int R_RAW = 4;         // packed batches in flight
 constexpr float R_TAU = 8.f;
 constexpr int R_PEXP = 7;        // numerators are at most 2^(R_PEXP + R_TAU) as fp16
-constexpr int R_EXPAND = 4;      // expanding warps of a kind: keys 8 .. 11, values 12 .. 15
-constexpr int R_MMA = 16, R_LOAD = 17, R_THREADS = 18 * 32;
+constexpr int R_GROUPS = 4;      // softmax groups of four warps, 0 .. 15
+constexpr int R_EXPAND = 4;      // expanding warps of a kind: keys 16 .. 19, values 20 .. 23
+constexpr int R_MMA = 24, R_LOAD = 25, R_THREADS = 26 * 32;
 constexpr int R_UNITS = 4;       // window batches whose exponents are kept
 constexpr uint32_t MAX_DOUBLED = 0x77ff;  // the largest half-precision number whose double is finite
 
@@ -81,7 +82,7 @@ __device__ __forceinline__ float2 halves_of(uint64_t a) {
   return d;
 }
 // barrier of the softmax warps
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;\n" ::: "memory"); }
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 512;\n" ::: "memory"); }
 // A warp's bounded wait.  What follows when the first look fails is out of line: most looks do not, and the kernel's roles
 // share an instruction cache.
 __device__ __noinline__ bool warp_wait_longer(uint32_t bar, uint32_t parity, volatile int* dead) {
@@ -170,8 +171,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   using Ly = RowsLayout<D, BK, BV, GS>;
   constexpr int NG = Ly::NG;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 2 + 2 * 4 + 8 + 2 * R_UNITS + 2];
-  __shared__ float half_sm[2][ROWS_TILE], m_sm[ROWS_TILE];  // largest element of half a row of q; softmax reference
+  __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 2 + 2 * 4 + 4 * R_GROUPS + 2 * R_UNITS + 2];
+  __shared__ float top_sm[R_GROUPS][ROWS_TILE], m_sm[ROWS_TILE];  // largest element of a quarter of a row of q; softmax reference
   __shared__ uint32_t unit_sm[R_UNITS][2][R_EXPAND];        // window batch, keys / values: largest magnitude of each expanding warp
   __shared__ uint32_t tmem_base_sm;
   __shared__ volatile int dead_sm;
@@ -189,8 +190,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   const uint32_t bar_s = bar_vfree + 8 * R_BUFS;         // [2] S of a batch is complete
   const uint32_t bar_p = bar_s + 16;                     // [2][2] the numerators of a batch's first / second tile are written
   const uint32_t bar_o = bar_p + 32;                     // [2][2] its value products are complete
-  const uint32_t bar_turn = bar_o + 32;                  // [4 warps][2] the reference for a first / second tile is there
-  const uint32_t bar_kunit = bar_turn + 64;              // [R_UNITS] the magnitudes of a window batch's keys are known
+  const uint32_t bar_turn = bar_o + 32;                  // [4 warps][R_GROUPS] the reference for a group's next tile is there
+  const uint32_t bar_kunit = bar_turn + 32 * R_GROUPS;              // [R_UNITS] the magnitudes of a window batch's keys are known
   const uint32_t bar_vunit = bar_kunit + 8 * R_UNITS;    // [R_UNITS] the same of its values
   const uint32_t bar_q = bar_vunit + 8 * R_UNITS;        // Q is written
   const uint32_t bar_end = bar_q + 8;                    // every product is complete
@@ -214,15 +215,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar_p + 8 * i, 4);
       mbar_init(bar_o + 8 * i, 1);
-      mbar_init(bar_turn + 16 * i, 1);
-      mbar_init(bar_turn + 16 * i + 8, 1);
+#pragma unroll
+      for (int k = 0; k < R_GROUPS; ++k) mbar_init(bar_turn + 8 * (R_GROUPS * i + k), 1);
     }
 #pragma unroll
     for (int i = 0; i < R_UNITS; ++i) {
       mbar_init(bar_kunit + 8 * i, R_EXPAND);
       mbar_init(bar_vunit + 8 * i, R_EXPAND);
     }
-    mbar_init(bar_q, 8);
+    mbar_init(bar_q, 4 * R_GROUPS);
     mbar_init(bar_end, 1);
     dead_sm = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -236,8 +237,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     const int x = row0 + k, h = x % G, ji = x / G, i = ji % p.each, j = ji / p.each;
     return ((size_t)j * (dm.B * p.each) + (size_t)u * p.each + i) * dm.Hq + hk * G + h;
   };
-  const int my_row = 16 * warp + (lane & 15);  // of q, for the warps that fetch it
-  const uint32_t my_call_row = warp < 8 && my_row < n_rows ? (uint32_t)call_row(my_row) : 0u;
+  const int my_row = 8 * warp + (lane & 7);  // of q, for the warps that fetch it
+  const uint32_t my_call_row = warp < 4 * R_GROUPS && my_row < n_rows ? (uint32_t)call_row(my_row) : 0u;
 
   // (tensor memory is asked for after the wait: a CTA of the preceding kernel that shares the SM may still have to get its own)
   grid_dependency_wait();
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     bulk_load(dst + Ly::RAW_VC, reinterpret_cast<const uint8_t*>(p.L.v_codes) + (size_t)bh * ((size_t)dm.nq_cap * (D * BV / 8)) + t * (16 * D * BV), 16 * D * BV, bar);
     bulk_load(dst + Ly::RAW_VM, reinterpret_cast<const uint8_t*>(p.L.v_meta) + (size_t)bh * ((size_t)dm.nq_cap * 4 * NG) + t * (RB * 4 * NG), RB * 4 * NG, bar);
   };
-  // Before the CTA's first barrier: the first packed batches, and q's rows into the second key operand's place, sixteen rows a
+  // Before the CTA's first barrier: the first packed batches, and q's rows into the second key operand's place, eight rows a
   // warp, lanes along a row.
   constexpr int QROW = 2 * D + 16;
   static_assert(ROWS_TILE * QROW <= Ly::KBYTES, "q fits");
@@ -282,18 +283,18 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     if (lane == 0)
       for (int i = 0; i < min(R_RAW, n_pk); ++i) load(i);
     __syncwarp();
-  } else if (warp < 8) {
-    constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES;
-    const int first = 16 * warp;
-    uint4 x[16 / AT_ONCE];
+  } else if (warp < 4 * R_GROUPS) {
+    constexpr int PIECES = D / 8, AT_ONCE = 32 / PIECES, ROWS = ROWS_TILE / (4 * R_GROUPS);
+    const int first = ROWS * warp;
+    uint4 x[ROWS / AT_ONCE];
 #pragma unroll
-    for (int k = 0; k < 16 / AT_ONCE; ++k) {
+    for (int k = 0; k < ROWS / AT_ONCE; ++k) {
       const int y = k * AT_ONCE + lane / PIECES;
       const uint32_t at = __shfl_sync(0xffffffffu, my_call_row, y);
       x[k] = first + y < n_rows ? reinterpret_cast<const uint4*>(p.q)[(size_t)at * PIECES + lane % PIECES] : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
-    for (int k = 0; k < 16 / AT_ONCE; ++k)
+    for (int k = 0; k < ROWS / AT_ONCE; ++k)
       sts128(q_sm + (first + k * AT_ONCE + lane / PIECES) * QROW + lane % PIECES * 16, x[k].x, x[k].y, x[k].z, x[k].w);
   }
 
@@ -372,10 +373,10 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       }
     }
     __syncwarp();
-  } else if (warp >= 8) {
-    // ================= expansion: keys (warps 8 .. 11), values (12 .. 15) =================
+  } else if (warp >= 4 * R_GROUPS) {
+    // ================= expansion: keys (warps 16 .. 19), values (20 .. 23) =================
     const int ew = warp & 3, o = lane & 3, sub = lane >> 2;  // a lane's sixteen elements of 64, and its row of eight
-    const bool keys = warp < 12;
+    const bool keys = warp < 4 * R_GROUPS + R_EXPAND;
     // Keys: 64 channels from 64 kb on of the 32 tokens of each of the slots slot0 .. slot0 + PARTS - 1.  Values: D / 4 channels
     // from v_c0 on, all of one channel group, of the tokens of either half of the batch.
     constexpr int PARTS = D / 64, STEPS = D / 32;
@@ -540,50 +541,46 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       }
     }
   } else {
-    // ================= softmax: group g takes tile g of every batch; thread = row =================
-    const int g = warp >> 2, quarter = warp & 3, k_row = tid & 127;
+    // ================= softmax: a group takes every fourth tile, one of every other batch; thread = row =================
+    const int group = warp >> 2, b = group >> 1, g = group & 1, quarter = warp & 3, k_row = tid & 127;
     const uint32_t row_t = tbase + ((uint32_t)(quarter * 32) << 16);
     const bool idle = 32 * quarter >= n_rows;  // none of this warp's rows exists
     float cq = p.scale * 1.4426950408889634f;
     {
-      // q: half of this thread's row as fp16 in the operands' order, bfloat16 scaled by a power of two into [1, 2), to tensor
-      // memory
-      uint4 x[D / 16];
+      // q: a quarter of this thread's row as fp16 in the operands' order, bfloat16 scaled by a power of two into [1, 2), to
+      // tensor memory
+      uint4 x[D / 32];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) x[i] = lds128(q_sm + k_row * QROW + g * D + 16 * i);
+      for (int i = 0; i < D / 32; ++i) x[i] = lds128(q_sm + k_row * QROW + group * (D / 2) + 16 * i);
       float f = 1.f;
       if (!p.f16) {
         uint32_t m = 0u;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) m = top_of(m, x[i]);
-        half_sm[g][k_row] = bf16_top(m);
+        for (int i = 0; i < D / 32; ++i) m = top_of(m, x[i]);
+        top_sm[group][k_row] = bf16_top(m);
         softmax_sync();
-        const float am = fmaxf(half_sm[0][k_row], half_sm[1][k_row]);
+        const float am = fmaxf(fmaxf(top_sm[0][k_row], top_sm[1][k_row]), fmaxf(top_sm[2][k_row], top_sm[3][k_row]));
         const int e = am > 0.f ? max(-100, min(100, -exponent_of(am))) : 0;
         f = pow2i(e);
         cq *= pow2i(-e);
       }
+      uint32_t y[D / 8];
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        uint32_t y[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 v = reorder8(x[4 * c + i], f, p.f16);
-          y[4 * i] = v.x; y[4 * i + 1] = v.y; y[4 * i + 2] = v.z; y[4 * i + 3] = v.w;
-        }
-        tmem_st<16>(row_t + Ly::COL_Q + g * (D / 4) + 16 * c, y);
+      for (int i = 0; i < D / 32; ++i) {
+        const uint4 v = reorder8(x[i], f, p.f16);
+        y[4 * i] = v.x; y[4 * i + 1] = v.y; y[4 * i + 2] = v.z; y[4 * i + 3] = v.w;
       }
+      tmem_st<D / 8>(row_t + Ly::COL_Q + group * (D / 8), y);
       tc_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_q);
     }
-    float m = -CUDART_INF_F;
-    int ev = 0;  // exponent of the values in O
+    const uint32_t s_t = row_t + Ly::COL_S + b * Ly::KN + g * RT;
+    const uint32_t my_turn = bar_turn + 8 * (R_GROUPS * quarter + group), next_turn = bar_turn + 8 * (R_GROUPS * quarter + (group + 1) % R_GROUPS);
 #pragma unroll 1
-    for (int i = 0; i < N; ++i) {
+    for (int i = b; i < N; i += 2) {
       const bool packed = i < n_pk;
-      const int b = i & 1;
       const uint32_t turn = (i >> 1) & 1;
       if (!warp_wait(bar_s + 8 * b, turn, &dead_sm)) break;
       if (!packed) {
@@ -591,23 +588,24 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         if (!warp_wait(bar_kunit + 8 * slot, round, &dead_sm) || !warp_wait(bar_vunit + 8 * slot, round, &dead_sm)) break;
       }
       tc_fence_after();
-      const uint32_t s_t = row_t + Ly::COL_S + b * Ly::KN + g * RT;
       const int n_valid = (packed ? n_q - (t_lo + i) * RB : r - (t_lo + i - pk_batches) * RB) - RT * g;  // of this tile
-      uint32_t s[2][32];
+      // 32 columns of S at a time, twice: for the search and for the numerators
+      auto columns = [&](int x, uint32_t (&s)[32]) {
+        tmem_ld<32>(s_t + 32 * x, s);
+        tc_wait_ld();
+        if (n_valid < 32 * x + 32) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (32 * x + k >= n_valid) s[k] = 0xff800000u;
+        }
+      };
       float c = cq, bias[2] = {0.f, 0.f}, xm = -CUDART_INF_F;
       if (!idle) {
-        uint32_t e[8];
-        tmem_ld<32>(s_t, s[0]);
-        tmem_ld<32>(s_t + 32, s[1]);
-        tmem_ld<8>(row_t + Ly::COL_S + b * Ly::KN + RB, e);
-        tc_wait_ld();
-        if (n_valid < RT) {
-#pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (k >= n_valid) s[k >> 5][k & 31] = 0xff800000u;
-        }
         // logits in log2 units: S c + bias of their 32 tokens
         if (packed) {
+          uint32_t e[8];
+          tmem_ld<8>(row_t + Ly::COL_S + b * Ly::KN + RB, e);
+          tc_wait_ld();
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const uint32_t z = g ? e[4 + 2 * x] : e[2 * x], y = g ? e[5 + 2 * x] : e[2 * x + 1];
@@ -618,28 +616,31 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          float a = __uint_as_float(s[x][0]), d = __uint_as_float(s[x][1]);
+          uint32_t s[32];
+          columns(x, s);
+          float a = __uint_as_float(s[0]), d = __uint_as_float(s[1]);
 #pragma unroll
           for (int k = 2; k < 30; k += 4) {
-            a = fmaxf(fmaxf(a, __uint_as_float(s[x][k])), __uint_as_float(s[x][k + 1]));
-            d = fmaxf(fmaxf(d, __uint_as_float(s[x][k + 2])), __uint_as_float(s[x][k + 3]));
+            a = fmaxf(fmaxf(a, __uint_as_float(s[k])), __uint_as_float(s[k + 1]));
+            d = fmaxf(fmaxf(d, __uint_as_float(s[k + 2])), __uint_as_float(s[k + 3]));
           }
-          a = fmaxf(fmaxf(a, __uint_as_float(s[x][30])), __uint_as_float(s[x][31]));
+          a = fmaxf(fmaxf(a, __uint_as_float(s[30])), __uint_as_float(s[31]));
           xm = fmaxf(xm, fmaf(fmaxf(a, d), c, bias[x]));
         }
       }
       // the reference that the tile before left
+      float m = -CUDART_INF_F;
       if (i > 0 || g > 0) {
-        if (!warp_wait(bar_turn + 16 * quarter + 8 * g, (g ? i : i - 1) & 1, &dead_sm)) break;
+        if (!warp_wait(my_turn, group > 0 ? turn : turn ^ 1u, &dead_sm)) break;
         m = m_sm[k_row];
       }
       const float m_old = m;
       if (xm > m + R_TAU || (m == -CUDART_INF_F && xm > m)) m = ceilf(xm);
       m_sm[k_row] = m;
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_turn + 16 * quarter + 8 * (1 - g));
-      const int e_new = packed ? 0 : batch_exponent(i, 1), de = g == 0 ? e_new - ev : 0;  // (for the second tile O has it already)
-      ev = e_new;
+      if (lane == 0) mbar_arrive(next_turn);
+      // the exponent of the values in O changes with a batch's first tile
+      const int de = packed || g > 0 ? 0 : batch_exponent(i, 1) - (i > n_pk ? batch_exponent(i - 1, 1) : 0);
       if ((i > 0 || g > 0) && !idle && __any_sync(0xffffffffu, m != m_old || de != 0)) {
         // O has to follow a raised reference, and the scale of the window's values: after the products of the tile before
         const int j = g ? i : i - 1;
@@ -661,13 +662,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         const uint64_t cc = pair_of(c, c);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+          uint32_t s[32];
+          columns(x, s);
           const float off = m == -CUDART_INF_F ? 0.f : bias[x] + ((float)R_PEXP - m);
           const uint64_t oo = pair_of(off, off);
           uint32_t y[16];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[x][4 * k]), __uint_as_float(s[x][4 * k + 1])), cc, oo));
-            const float2 d = halves_of(fma2(pair_of(__uint_as_float(s[x][4 * k + 2]), __uint_as_float(s[x][4 * k + 3])), cc, oo));
+            const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[4 * k]), __uint_as_float(s[4 * k + 1])), cc, oo));
+            const float2 d = halves_of(fma2(pair_of(__uint_as_float(s[4 * k + 2]), __uint_as_float(s[4 * k + 3])), cc, oo));
             y[2 * k] = pack_io2<true>(ex2(a.x), ex2(d.x));
             y[2 * k + 1] = pack_io2<true>(ex2(a.y), ex2(d.y));
           }
@@ -680,11 +683,12 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       if (lane == 0) mbar_arrive(bar_p + 16 * b + 8 * g);
     }
 
-    // ---- the result, or the split's partial: each group takes half of the channels ----
+    // ---- the result, or the split's partial: each group takes a quarter of the channels ----
     if (N > 0) mbar_wait(bar_end, 0, &dead_sm);
     softmax_sync();  // (every warp comes here, whatever failed)
     tc_fence_after();
-    if (N > 0) m = m_sm[k_row];
+    float m = N > 0 ? m_sm[k_row] : -CUDART_INF_F;
+    const int ev = N > n_pk ? batch_exponent(N - 1, 1) : 0;
     const float unit = pow2i(-R_PEXP), uv = unit * pow2i(-ev);
     float l = 0.f, extra[NG];
     {
@@ -703,8 +707,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     // through shared memory (the operands' place), so that a row leaves in one piece
     const uint32_t row_bytes = wide ? 4 * D : 2 * D, mine = sm + k_row * (row_bytes + 16);
 #pragma unroll 1
-    for (int k = 0; k < D / 2; k += 16) {
-      const int c0 = g * (D / 2) + k;
+    for (int k = 0; k < D / 4; k += 16) {
+      const int c0 = group * (D / 4) + k;
       uint32_t y[16];
       tmem_ld<16>(row_t + Ly::COL_O + c0, y);
       tc_wait_ld();
@@ -727,7 +731,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     }
     proxy_fence();
     softmax_sync();
-    if (g == 0 && store) {
+    if (group == 0 && store) {
       const size_t to_row = call_row(k_row);
       uint8_t* const to = p.part_acc != nullptr ? reinterpret_cast<uint8_t*>(p.part_acc + (to_row * p.ns + split) * D)
                                                 : reinterpret_cast<uint8_t*>(p.out) + to_row * row_bytes;
