@@ -549,7 +549,11 @@ int ensure_clean_scratch(xq_cache* c, cudaStream_t st) {
   cudaError_t e = cudaMemsetAsync(c->ws + c->plan.tickets, 0, (size_t)dm.B * dm.Hkv * DECODE_MAX_LAYERS * 4, st);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->ws + c->plan.status, 0, 4, st);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  c->tickets_clean = true;
+  // (a call that is captured clears them when its graph runs, which may be never: the next one clears them too)
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  e = cudaStreamIsCapturing(st, &capture);
+  if (e != cudaSuccess) return fail_cuda(c, e);
+  c->tickets_clean = capture == cudaStreamCaptureStatusNone;
   return XQ_OK;
 }
 

@@ -123,11 +123,36 @@ __device__ __forceinline__ uint32_t code_times(uint32_t w, int j, uint32_t s) {
   const uint32_t less = (base | 0x80008000u) + (BITS == 2 ? 0x00010001u << (2 * j) : 0u);  // and one more for two bits
   return hmul2(hadd2((w & field) | base, less), s);
 }
-template <int BITS>
+template <int OFF>
+__device__ __forceinline__ void sts128_at(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0 + %5], {%1,%2,%3,%4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w), "n"(OFF) : "memory");
+}
+template <int OFF>
+__device__ __forceinline__ uint32_t lds32_at(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1 + %2];\n" : "=r"(v) : "r"(a), "n"(OFF) : "memory");
+  return v;
+}
+template <int BITS, int OFF>
 __device__ __forceinline__ void expand16(uint32_t w, const uint4& s0, const uint4& s1, uint32_t dst0, uint32_t dst1) {
   const uint32_t y = w >> 8;
-  sts128(dst0, code_times<BITS>(w, 0, s0.x), code_times<BITS>(y, 0, s0.y), code_times<BITS>(w, 1, s0.z), code_times<BITS>(y, 1, s0.w));
-  sts128(dst1, code_times<BITS>(w, 2, s1.x), code_times<BITS>(y, 2, s1.y), code_times<BITS>(w, 3, s1.z), code_times<BITS>(y, 3, s1.w));
+  sts128_at<OFF>(dst0, code_times<BITS>(w, 0, s0.x), code_times<BITS>(y, 0, s0.y), code_times<BITS>(w, 1, s0.z), code_times<BITS>(y, 1, s0.w));
+  sts128_at<OFF>(dst1, code_times<BITS>(w, 2, s1.x), code_times<BITS>(y, 2, s1.y), code_times<BITS>(w, 3, s1.z), code_times<BITS>(y, 3, s1.w));
+}
+// N rows of them, eight rows apart (1024 bytes of the operand), packed words STRIDE bytes apart; shift: of 1-bit codes' words
+template <int N, int STRIDE, int K = 0>
+__device__ __forceinline__ void load_codes(uint32_t src, uint32_t (&w)[N]) {
+  if constexpr (K < N) {
+    w[K] = lds32_at<K * STRIDE>(src);
+    load_codes<N, STRIDE, K + 1>(src, w);
+  }
+}
+template <int BITS, int N, int K = 0>
+__device__ __forceinline__ void expand_rows(const uint32_t (&w)[N], int shift, const uint4& s0, const uint4& s1, uint32_t dst0, uint32_t dst1) {
+  if constexpr (K < N) {
+    expand16<BITS, 1024 * K>(BITS == 2 ? w[K] : w[K] >> shift, s0, s1, dst0, dst1);
+    expand_rows<BITS, N, K + 1>(w, shift, s0, s1, dst0, dst1);
+  }
 }
 // Eight of them where a scale is too large to be doubled: c s + z, rounded (the operand's extra rows are then zero).  w:
 // shifted so that the first field is at bit 0; s_at, z_at: where the parameters of element j are in shared memory.
@@ -392,6 +417,10 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
                                    : Ly::RAW_VC + (BV == 2 ? o * 4 : o / 2 * 4) + (v_c0 + sub) * 16;
     const uint32_t meta_off = keys ? Ly::RAW_KM + 2 * (lane * (D / 32) + 2 * kb) : Ly::RAW_VM + lane * (4 * NG) + 2 * vg;
     const uint32_t op_off = keys ? kb * Ly::KBLOCK : Ly::OFF_V;
+    const int at = (lane & ~3) | ((lane & 1) << 1) | ((lane >> 1) & 1);  // place of channel `lane`: elements of four 0, 2, 1, 3
+    const uint32_t params_off = keys ? piece_at(rz, at >> 3) + 2 * (at & 7) : piece_at(lane & 2 ? rz : rs, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;
+    const uint32_t row_off = piece_at(row, 2 * o), scales_off = piece_at(rs, 2 * o);
+    static_assert(PARTS <= 2 && RB % 8 == 0, "rows rz + 2 x: bit 1 of rz is clear where x can be 1");
     if (!keys && ew < 2 && lane < 8) {  // the row that sums the numerators
       for (int b = 0; b < R_BUFS; ++b)
         sts128(sm + Ly::OFF_V + b * Ly::VBYTES + ew * Ly::VBLOCK + piece_at(Ly::ONES, lane), 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
@@ -412,25 +441,23 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         for (int x = 0; x < PARTS; ++x) {
           const uint32_t src = raw + code_off + x * (32 * Ly::KROW);
           uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) codes[k] = lds32(src + 8 * k * CB);
+          load_codes<4, 8 * CB>(src, codes);
           // parameters of channels 64 kb + lane and 32 more, side by side in the group's order
           const uint32_t meta = raw + meta_off + (slot0 + x) * 32 / GS * (4 * D);
           uint32_t sw = lds32(meta), zw = lds32(meta + 2 * D);
           const bool large = BK == 2 && __any_sync(0xffffffffu, (sw & 0xffffu) > MAX_DOUBLED || (sw >> 16) > MAX_DOUBLED);
           if (large) sw = zw = 0u;
-          const int at = (lane & ~3) | ((lane & 1) << 1) | ((lane >> 1) & 1);  // elements of four: 0, 2, 1, 3
-          const uint32_t to_z = dst + piece_at(rz + 2 * x, at >> 3) + 2 * (at & 7), to_s = dst + piece_at(rs + 2 * x, at >> 3) + 2 * (at & 7);
+          // (rows rz + 2 x and the one after it: bits of a row's number are exclusive-ored into the place of its pieces)
+          const uint32_t to_z = ((dst + params_off) ^ (32u * x)) + 256u * x, to_s = (to_z ^ 16u) + 128u;
           sts16(to_z, zw & 0xffffu);
           sts16(to_z ^ 64u, zw >> 16);  // four pieces on
           sts16(to_s, sw & 0xffffu);
           sts16(to_s ^ 64u, sw >> 16);
           __syncwarp();
-          const uint32_t d0 = dst + piece_at(row + 32 * x, 2 * o), d1 = d0 ^ 16u, s_row = dst + piece_at(rs + 2 * x, 2 * o);
+          const uint32_t d0 = dst + row_off + 4096u * x, d1 = d0 ^ 16u, s_row = ((dst + scales_off) ^ (32u * x)) + 256u * x;
           if (!large) {
             const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) expand16<BK>(codes[k] >> shift, s0, s1, d0 + 1024 * k, d1 + 1024 * k);
+            expand_rows<BK, 4>(codes, shift, s0, s1, d0, d1);
           } else {
             const uint32_t group = raw + Ly::RAW_KM + (slot0 + x) * 32 / GS * (4 * D);
 #pragma unroll 1
@@ -447,8 +474,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         for (int x = 0; x < 2; ++x) {
           const uint32_t src = raw + code_off + x * (BV == 2 ? D * 16 : 8), block = dst + x * Ly::VBLOCK;
           uint32_t codes[STEPS];
-#pragma unroll
-          for (int k = 0; k < STEPS; ++k) codes[k] = lds32(src + 128 * k);
+          load_codes<STEPS, 128>(src, codes);
           // Parameters of token `lane` and of lane + 32 of the half, (scale, zero-point); none of tokens that do not exist.  A
           // word of the operand's rows has tokens (t, t + 2): one of the two lanes writes the scales, the other the zero-points.
           const uint32_t meta = raw + meta_off + x * (64 * 4 * NG);
@@ -460,7 +486,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             if (64 * x + lane + 32 >= valid) sz[1] = 0u;
           }
           const bool large = BV == 2 && __any_sync(0xffffffffu, (sz[0] & 0xffffu) > MAX_DOUBLED || (sz[1] & 0xffffu) > MAX_DOUBLED);
-          const uint32_t to = block + piece_at(lane & 2 ? rz : rs, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;
+          const uint32_t to = block + params_off;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2);
@@ -468,11 +494,10 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             sts32(to ^ (64u * k), large ? 0u : w);
           }
           __syncwarp();
-          const uint32_t d0 = block + piece_at(row, 2 * o), d1 = d0 ^ 16u, s_row = block + piece_at(rs, 2 * o);
+          const uint32_t d0 = block + row_off, d1 = d0 ^ 16u, s_row = block + scales_off;
           if (!large) {
             const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
-#pragma unroll
-            for (int k = 0; k < STEPS; ++k) expand16<BV>(codes[k] >> shift, s0, s1, d0 + 1024 * k, d1 + 1024 * k);
+            expand_rows<BV, STEPS>(codes, shift, s0, s1, d0, d1);
           } else {
             // (a token that does not exist stands for the last one that does: its numerator is zero)
 #pragma unroll 1

@@ -269,6 +269,14 @@ def test_prefix_of_its_own(shape, S, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[6]])
+def test_prefix_behind_long_tails(shape):
+    # the sequences' own tokens in several splits: one token (decode kernels) and twenty (chunk kernel)
+    _prefix_case(shape, xq.XQ_KERNEL_AUTO, 1, 2, 100, 1500, 1)
+    _prefix_case(shape, xq.XQ_KERNEL_AUTO, 1, 2, 100, 1500, 20)
+
+
+@pytest.mark.gpu
 def test_prefix_more_rows_than_a_tile():
     # 3 sequences x 20 tokens x 4 heads = 240 rows; 23 x 12 = 276
     _prefix_case(SHAPES[0], xq.XQ_KERNEL_AUTO, 1, 3, 300, 20, 20)
@@ -557,6 +565,23 @@ def test_calls_on_other_streams_and_in_a_graph():
         assert torch.equal(outs[1], cache.cross_attention(1, q, lengths=lengths))
         x = _queries(four, 30, 1)[0].to(DEV)
         assert torch.equal(spare.decode_attention(0, x[index.long()].contiguous()), cache.decode_attention(0, x)[index.long()])
+    cache.check_device()
+
+
+@pytest.mark.gpu
+def test_first_call_of_a_handle_in_a_graph_that_never_runs():
+    # the handle's counters are cleared by a first call; one that is only captured does not count
+    cfg = _config(batch=2, max_seq=2000)
+    K, V = _tokens(cfg, 1, 1500)
+    q = _queries(cfg, 2, 1).to(DEV)
+    want = _filled(cfg, K, V).cross_attention(0, q)
+    cache = _filled(cfg, K, V)
+    cache.workspace[xq.xq_region(cache.handle, 1, 3)[1] + xq.xq_region(cache.handle, 1, 3)[2] * 4:].fill_(0xff)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.cross_attention(0, q)
+    assert torch.equal(cache.cross_attention(0, q), want)
     cache.check_device()
 
 
