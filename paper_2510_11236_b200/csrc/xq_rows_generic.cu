@@ -82,47 +82,58 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) rows_generic_kernel(const __gr
 }
 
 // out = (sum_s acc_s 2^(m_s - M) + own 2^(lse - M)) / (sum_s l_s 2^(m_s - M) + 2^(lse - M)): a part without tokens has
-// m = -infinity and counts nothing.  A warp takes a row, a lane D / 32 neighbouring channels.
+// m = -infinity and counts nothing.  A warp takes a row, a lane D / 32 neighbouring channels.  Bound: trips to L2; the sums of the
+// first JOIN_SPLITS splits are asked for together with the references, so that most calls make one.
+constexpr int JOIN_SPLITS = 16;
 template <int DPL>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinParams p) {
   constexpr int D = DPL * 32;
   grid_dependents_go();
-  grid_dependency_wait();
   const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
-  if (row >= p.rows) return;
   const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row * p.ns;
   const float* acc = p.part_acc + row * p.ns * D + lane * DPL;
+  grid_dependency_wait();
+  if (row >= p.rows) return;
   const float lse = p.own != nullptr ? p.own_lse[row] : -CUDART_INF_F;
-  float M = lse;
   auto state = [&](int s) { return p.part_lse != nullptr ? make_float2(p.part_lse[row], 1.f) : ml[s]; };
-  for (int s = lane; s < p.ns; s += 32) M = fmaxf(M, state(s).x);
+  float2 x[JOIN_SPLITS];
+  float v[JOIN_SPLITS][DPL];
+  auto fetch = [&](int s0) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  float a[DPL], L = 0.f;
-#pragma unroll
-  for (int j = 0; j < DPL; ++j) a[j] = 0.f;
-  auto add = [&](float m, float l, const float* v) {
-    const bool none = m == -CUDART_INF_F;  // v is then not defined
-    const float f = exp2f(m - M);
-    L = none ? L : fmaf(l, f, L);
-#pragma unroll
-    for (int j = 0; j < DPL; ++j) a[j] = none ? a[j] : fmaf(v[j], f, a[j]);
-  };
-  // eight splits' loads at a time: a trip to L2 for each eight
-  for (int s0 = 0; s0 < p.ns; s0 += 8) {
-    float2 x[8];
-    float v[8][DPL];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < JOIN_SPLITS; ++k) {
       const bool there = s0 + k < p.ns;
       x[k] = there ? state(s0 + k) : make_float2(-CUDART_INF_F, 0.f);
 #pragma unroll
       for (int j = 0; j < DPL; j += 2)
         *reinterpret_cast<float2*>(&v[k][j]) = there ? *reinterpret_cast<const float2*>(acc + (size_t)(s0 + k) * D + j) : make_float2(0.f, 0.f);
     }
+  };
+  fetch(0);
+  float M = lse;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) add(x[k].x, x[k].y, v[k]);
+  for (int k = 0; k < JOIN_SPLITS; ++k) M = fmaxf(M, x[k].x);
+  if (p.ns > JOIN_SPLITS) {
+    for (int s = JOIN_SPLITS + lane; s < p.ns; s += 32) M = fmaxf(M, ml[s].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  }
+  float a[DPL], L = 0.f;
+#pragma unroll
+  for (int j = 0; j < DPL; ++j) a[j] = 0.f;
+  auto add = [&](float m, float l, const float* y) {
+    const bool none = m == -CUDART_INF_F;  // the sums are then not defined
+    const float f = exp2f(m - M);
+    L = none ? L : fmaf(l, f, L);
+#pragma unroll
+    for (int j = 0; j < DPL; ++j) a[j] = none ? a[j] : fmaf(y[j], f, a[j]);
+  };
+  for (int s0 = 0;;) {
+#pragma unroll
+    for (int k = 0; k < JOIN_SPLITS; ++k) add(x[k].x, x[k].y, v[k]);
+    s0 += JOIN_SPLITS;
+    if (s0 >= p.ns) break;
+    fetch(s0);
   }
   if (p.own != nullptr) {
     float v[DPL];
