@@ -174,14 +174,14 @@ def _reference(q, part, own, scale, seen_own):
     return out, off + 1e-6 * np.abs(out)
 
 
-def _check(cfg, out32, out16, q, restore_part, restore_own, T, own_len, heads=None):
-    """Every row of the sequences and heads against the reference.  restore_*(b, h): the stream's tokens."""
+def _check(cfg, out32, out16, q, restore_part, restore_own, T, own_len, heads=None, batch=None):
+    """Every row of the sequences and heads (all, or those named) against the reference.  restore_*(b, h): the stream's tokens."""
     B, G = q.shape[1], cfg.n_q_heads // cfg.n_kv_heads
     scale = cfg.sm_scale if cfg.sm_scale > 0 else 1 / math.sqrt(cfg.head_dim)
     o32, o16, qd = out32.double().cpu().numpy(), out16.double().cpu().numpy(), q.double().cpu().numpy()
     half = torch.finfo(q.dtype).eps / 2
     worst = 0.0
-    for b in range(B):
+    for b in range(B) if batch is None else batch:
         for h in range(cfg.n_kv_heads) if heads is None else heads:
             part, own = restore_part(b, h), restore_own(b, h)
             for j in range(T):
@@ -363,6 +363,52 @@ def test_cross_masked_tokens_that_are_not_finite(kernel, bad, T):
 def test_cross_many_rows():
     _cross_case(SHAPES[2], xq.XQ_KERNEL_AUTO, 1, 260, 300)
     _cross_case(SHAPES[0], xq.XQ_KERNEL_AUTO, 2, 130, 65, lengths=[130, 41])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,T,f16,ragged", [(16, 40, False, True), (6, 40, False, False), (13, 33, True, True), (40, 33, False, False)])
+def test_cross_more_tiles_than_half_the_device(B, T, f16, ragged):
+    # several waves of CTAs.  Some streams against the reference, all against the scalar kernel: off by at most 2^-11 of the
+    # values' spread, and by little more.
+    kw = dict(batch=B, n_q_heads=32, n_kv_heads=8, max_seq=700, vq=0, io_dtype=int(f16))
+    cfg, other = _config(**kw), _config(kernel=xq.XQ_KERNEL_GENERIC, **kw)
+    K, V = _tokens(cfg, B, 700)
+    cache, slow = _filled(cfg, K, V), _filled(other, K, V)
+    n = np.random.default_rng(B).integers(0, 701, B) if ragged else np.full(B, 700)
+    n[0], n[1] = (0, 700) if ragged else (700, 700)
+    lengths = torch.tensor(n, dtype=torch.int32, device=DEV) if ragged else None
+    q = _queries(cfg, 3, T)
+    o32, o16 = cache.cross_attention(1, q.to(DEV), lengths=lengths, f32=True), cache.cross_attention(1, q.to(DEV), lengths=lengths)
+    want = slow.cross_attention(1, q.to(DEV), lengths=lengths, f32=True)
+    assert (o32 - want).abs().max() <= 2.0 ** -11 * 2 * V[1].abs().max().item() * 1.1
+    none = [np.zeros((0, 128))] * 4
+    for b, h in ((1, 0), (B - 1, 7), (B // 2, 3)):
+        _check(cfg, o32, o16, q, lambda b, h: [x[:n[b]] for x in _restored(cfg, K, V, 1, b, h)], lambda b, h: none, T, 0, heads=[h], batch=[b])
+    cache.check_device()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,P", [(SHAPES[0], 1), (SHAPES[3], 5)])
+def test_prefix_more_tiles_than_half_the_device(shape, P):
+    # 8 sequences of 40 tokens behind each prompt, eight kv heads
+    D, Hq, Hkv, g, R, kq, vq, f16 = shape
+    shape = (D, 32, 8, g, R, kq, vq, f16)
+    cp, cc = _shape(shape, batch=P, max_seq=900), _shape(shape, batch=8 * P, max_seq=80)
+    kp, vp = _tokens(cp, 1, 900)
+    ko, vo = _tokens(cc, 2, 55)
+    prefix, cache = _filled(cp, kp, vp), _filled(cc, ko, vo)
+    q = _queries(cc, 3, 40)
+    o32, o16 = cache.prefix_attention(prefix, 0, q.to(DEV), f32=True), cache.prefix_attention(prefix, 0, q.to(DEV))
+    for b, h in ((0, 0), (8 * P - 1, 7), (3, 5)):
+        _check(cc, o32, o16, q, lambda b, h: _restored(cp, kp, vp, 0, b // 8, h), lambda b, h: _restored(cc, ko, vo, 0, b, h), 40, 55,
+               heads=[h], batch=[b])
+    # without own tokens
+    alone = xq.Cache(cc, DEV)
+    o32, o16 = alone.prefix_attention(prefix, 1, q.to(DEV), f32=True), alone.prefix_attention(prefix, 1, q.to(DEV))
+    none = [np.zeros((0, D))] * 4
+    for b, h in ((0, 0), (8 * P - 1, 7), (3, 5)):
+        _check(cc, o32, o16, q, lambda b, h: _restored(cp, kp, vp, 1, b // 8, h), lambda b, h: none, 40, 0, heads=[h], batch=[b])
+    cache.check_device()
 
 
 # ---- gathered sequences ----
