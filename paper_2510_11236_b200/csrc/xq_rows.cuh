@@ -81,6 +81,10 @@ __device__ __forceinline__ float2 halves_of(uint64_t a) {
   asm("mov.b64 {%0, %1}, %2;\n" : "=f"(d.x), "=f"(d.y) : "l"(a));
   return d;
 }
+// one lane's arrival, without a branch
+__device__ __forceinline__ void arrive_if(bool p, uint32_t bar) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar), "r"((uint32_t)p) : "memory");
+}
 // barrier of the softmax warps
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 512;\n" ::: "memory"); }
 // A warp's bounded wait.  What follows when the first look fails is out of line: most looks do not, and the kernel's roles
@@ -90,6 +94,12 @@ __device__ __noinline__ bool warp_wait_longer(uint32_t bar, uint32_t parity, vol
 }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
   return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) != 0u) || warp_wait_longer(bar, parity, dead);
+}
+
+// two of them, looked at together
+__device__ __forceinline__ bool warp_wait_both(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int* dead) {
+  const uint32_t there0 = mbar_try_wait(bar0, parity0), there1 = mbar_try_wait(bar1, parity1);
+  return __all_sync(0xffffffffu, (there0 & there1) != 0u) || (warp_wait_longer(bar0, parity0, dead) && warp_wait_longer(bar1, parity1, dead));
 }
 
 template <int D, int BK, int BV, int GS>
@@ -431,31 +441,51 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     for (int i = 0; i < N; ++i) {
       const int b = i & 1;
       const bool packed = i < n_pk;
-      if (packed && !warp_wait(bar_rfull + 8 * (i % R_RAW), (i / R_RAW) & 1, &dead_sm)) break;
-      if (keys && i == 1 && !warp_wait(bar_q, 0, &dead_sm)) break;  // (q lies there until then)
-      if (i >= R_BUFS && !warp_wait((keys ? bar_kfree : bar_vfree) + 8 * b, ((i >> 1) & 1) ^ 1, &dead_sm)) break;
+      {
+        // the batch's packed data, and the operand's place: free, and for the second keys not q's any more
+        const uint32_t bar_raw = bar_rfull + 8 * (i % R_RAW), raw_turn = (i / R_RAW) & 1;
+        const uint32_t bar_free = i >= R_BUFS ? (keys ? bar_kfree : bar_vfree) + 8 * b : bar_q;
+        const uint32_t free_turn = i >= R_BUFS ? ((i >> 1) & 1) ^ 1 : 0u;
+        const bool waits = i >= R_BUFS || (keys && i == 1);
+        if (packed && waits) {
+          if (!warp_wait_both(bar_raw, raw_turn, bar_free, free_turn, &dead_sm)) break;
+        } else {
+          if (packed && !warp_wait(bar_raw, raw_turn, &dead_sm)) break;
+          if (waits && !warp_wait(bar_free, free_turn, &dead_sm)) break;
+        }
+      }
       const uint32_t raw = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW;
       const uint32_t dst = sm + op_off + b * (keys ? Ly::KBYTES : Ly::VBYTES);
       if (packed && keys) {
+        // parameters of channels 64 kb + lane and 32 more, side by side in the group's order, to the operand's rows
+        uint32_t sw[PARTS], zw[PARTS], large = 0u;  // bit x: of slot x
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) {
+          const uint32_t meta = raw + meta_off + (slot0 + x) * 32 / GS * (4 * D);
+          sw[x] = lds32(meta);
+          zw[x] = lds32_at<2 * D>(meta);
+        }
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) {
+          if (BK == 2 && __any_sync(0xffffffffu, (sw[x] & 0xffffu) > MAX_DOUBLED || (sw[x] >> 16) > MAX_DOUBLED)) {
+            large |= 1u << x;
+            sw[x] = zw[x] = 0u;
+          }
+          // (rows rz + 2 x and the one after it: bits of a row's number are exclusive-ored into the place of its pieces)
+          const uint32_t to_z = ((dst + params_off) ^ (32u * x)) + 256u * x, to_s = (to_z ^ 16u) + 128u;
+          sts16(to_z, zw[x] & 0xffffu);
+          sts16(to_z ^ 64u, zw[x] >> 16);  // four pieces on
+          sts16(to_s, sw[x] & 0xffffu);
+          sts16(to_s ^ 64u, sw[x] >> 16);
+        }
+        __syncwarp();
 #pragma unroll 1
         for (int x = 0; x < PARTS; ++x) {
           const uint32_t src = raw + code_off + x * (32 * Ly::KROW);
-          uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
-          load_codes<4, 8 * CB>(src, codes);
-          // parameters of channels 64 kb + lane and 32 more, side by side in the group's order
-          const uint32_t meta = raw + meta_off + (slot0 + x) * 32 / GS * (4 * D);
-          uint32_t sw = lds32(meta), zw = lds32(meta + 2 * D);
-          const bool large = BK == 2 && __any_sync(0xffffffffu, (sw & 0xffffu) > MAX_DOUBLED || (sw >> 16) > MAX_DOUBLED);
-          if (large) sw = zw = 0u;
-          // (rows rz + 2 x and the one after it: bits of a row's number are exclusive-ored into the place of its pieces)
-          const uint32_t to_z = ((dst + params_off) ^ (32u * x)) + 256u * x, to_s = (to_z ^ 16u) + 128u;
-          sts16(to_z, zw & 0xffffu);
-          sts16(to_z ^ 64u, zw >> 16);  // four pieces on
-          sts16(to_s, sw & 0xffffu);
-          sts16(to_s ^ 64u, sw >> 16);
-          __syncwarp();
           const uint32_t d0 = dst + row_off + 4096u * x, d1 = d0 ^ 16u, s_row = ((dst + scales_off) ^ (32u * x)) + 256u * x;
-          if (!large) {
+          if (BK == 1 || !((large >> x) & 1u)) {
+            uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
+            load_codes<4, 8 * CB>(src, codes);
             const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
             expand_rows<BK, 4>(codes, shift, s0, s1, d0, d1);
           } else {
@@ -470,32 +500,32 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         }
       } else if (packed) {
         const int valid = n_q - (t_lo + i) * RB;  // tokens of the batch that exist
+        // Parameters of tokens lane, lane + 32, + 64, + 96, (scale, zero-point); none of tokens that do not exist.  A word of the
+        // operand's rows has tokens (t, t + 2): one of the two lanes writes the scales, the other the zero-points.
+        uint32_t sz[4], large = 0u;  // bit x: of half x
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sz[k] = lds16(raw + meta_off + k * (128 * NG)) | lds16(raw + meta_off + k * (128 * NG) + 2 * NG) << 16;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (valid < RB && lane + 32 * k >= valid) sz[k] = 0u;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (BV == 2 && __any_sync(0xffffffffu, (sz[2 * x] & 0xffffu) > MAX_DOUBLED || (sz[2 * x + 1] & 0xffffu) > MAX_DOUBLED)) large |= 1u << x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2);
+          const uint32_t w = lane & 2 ? __byte_perm(other, sz[k], 0x7632) : __byte_perm(sz[k], other, 0x5410);
+          sts32((dst + params_off + (k >> 1) * Ly::VBLOCK) ^ (64u * (k & 1)), (large >> (k >> 1)) & 1u ? 0u : w);
+        }
+        __syncwarp();
 #pragma unroll 1
         for (int x = 0; x < 2; ++x) {
           const uint32_t src = raw + code_off + x * (BV == 2 ? D * 16 : 8), block = dst + x * Ly::VBLOCK;
-          uint32_t codes[STEPS];
-          load_codes<STEPS, 128>(src, codes);
-          // Parameters of token `lane` and of lane + 32 of the half, (scale, zero-point); none of tokens that do not exist.  A
-          // word of the operand's rows has tokens (t, t + 2): one of the two lanes writes the scales, the other the zero-points.
-          const uint32_t meta = raw + meta_off + x * (64 * 4 * NG);
-          uint32_t sz[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) sz[k] = lds16(meta + k * (128 * NG)) | lds16(meta + k * (128 * NG) + 2 * NG) << 16;
-          if (valid < RB) {
-            if (64 * x + lane >= valid) sz[0] = 0u;
-            if (64 * x + lane + 32 >= valid) sz[1] = 0u;
-          }
-          const bool large = BV == 2 && __any_sync(0xffffffffu, (sz[0] & 0xffffu) > MAX_DOUBLED || (sz[1] & 0xffffu) > MAX_DOUBLED);
-          const uint32_t to = block + params_off;
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2);
-            const uint32_t w = lane & 2 ? __byte_perm(other, sz[k], 0x7632) : __byte_perm(sz[k], other, 0x5410);
-            sts32(to ^ (64u * k), large ? 0u : w);
-          }
-          __syncwarp();
           const uint32_t d0 = block + row_off, d1 = d0 ^ 16u, s_row = block + scales_off;
-          if (!large) {
+          if (BV == 1 || !((large >> x) & 1u)) {
+            uint32_t codes[STEPS];
+            load_codes<STEPS, 128>(src, codes);
             const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
             expand_rows<BV, STEPS>(codes, shift, s0, s1, d0, d1);
           } else {
@@ -560,10 +590,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       }
       proxy_fence();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive((keys ? bar_kfull : bar_vfull) + 8 * b);
-        if (packed) mbar_arrive(bar_rfree + 8 * (i % R_RAW));
-      }
+      arrive_if(lane == 0, (keys ? bar_kfull : bar_vfull) + 8 * b);
+      arrive_if(lane == 0 && packed, bar_rfree + 8 * (i % R_RAW));
     }
   } else {
     // ================= softmax: a group takes every fourth tile, one of every other batch; thread = row =================
@@ -663,7 +691,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       if (xm > m + R_TAU || (m == -CUDART_INF_F && xm > m)) m = ceilf(xm);
       m_sm[k_row] = m;
       __syncwarp();
-      if (lane == 0) mbar_arrive(next_turn);
+      arrive_if(lane == 0, next_turn);
       // the exponent of the values in O changes with a batch's first tile
       const int de = packed || g > 0 ? 0 : batch_exponent(i, 1) - (i > n_pk ? batch_exponent(i - 1, 1) : 0);
       if ((i > 0 || g > 0) && !idle && __any_sync(0xffffffffu, m != m_old || de != 0)) {
@@ -705,7 +733,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 16 * b + 8 * g);
+      arrive_if(lane == 0, bar_p + 16 * b + 8 * g);
     }
 
     // ---- the result, or the split's partial: each group takes a quarter of the channels ----
