@@ -269,9 +269,9 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, const DecodeLay
 // out = sum_s acc_s 2^(m_s-M) / sum_s l_s 2^(m_s-M).  No CTA ever waits for another.
 // What it takes is two trips to L2, one for all (m, l) and one for the partials: a warp that went through its share of
 // the heads one after the other, both trips for each, made it 2.3 us with four heads and 5.1 us with eight.
-// L, part_acc, part_ml: of the first of the CTA's NL layers; weights: NL * G * (ns + 1) floats of shared memory.  RAGGED: a
+// L, part_acc, part_ml: of the first of the CTA's NL layers; weights: NL * G * (ns + 1) floats of shared memory.  SHARED: a
 // stream may have no token at all, its result is zero.
-template <int NL, bool RAGGED>
+template <int NL, bool SHARED>
 __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const DecodeLayer* L, int ns, int hk, int b,
                                              const float* part_acc, const float* part_ml, unsigned* ticket, int* s_flag,
                                              float* weights) {
@@ -301,7 +301,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       M = x.x;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = lane < ns && !(RAGGED && x.x == -CUDART_INF_F) ? ex2(x.x - M) : 0.f;
+      const float f = lane < ns && !(SHARED && x.x == -CUDART_INF_F) ? ex2(x.x - M) : 0.f;
       Ls = x.y * f;
       if (lane < ns) w[lane] = f;
     } else {
@@ -310,7 +310,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       for (int s = lane; s < ns; s += 32) {
         const float2 x = ld_cg2(ml + 2 * s);
-        const float f = RAGGED && x.x == -CUDART_INF_F ? 0.f : ex2(x.x - M);
+        const float f = SHARED && x.x == -CUDART_INF_F ? 0.f : ex2(x.x - M);
         Ls = fmaf(x.y, f, Ls);
         w[s] = f;
       }
@@ -318,8 +318,8 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
     if (lane == 0) {
-      w[ns] = RAGGED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
-      if (NL == 1 && p.lse != nullptr) p.lse[row_of(v)] = M + log2f(Ls);
+      w[ns] = SHARED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
+      if (NL == 1 && p.lse != nullptr) p.lse[SHARED ? shared_row(dm, p.each, b, hk, v) : row_of(v)] = M + log2f(Ls);
     }
   }
   __syncthreads();
@@ -343,12 +343,12 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
     }
     const float inv = w[ns];
     const int l = NL == 1 || v < dm.G ? 0 : 1;
-    store_out(p, L[l], hq0 + (v - l * dm.G), c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+    store_out(p, L[l], SHARED ? shared_row(dm, p.each, b, hk, v) : hq0 + (v - l * dm.G), c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
   }
   if (threadIdx.x == 0) *ticket = 0u;  // ready for the next launch on this stream
 }
 
-template <int BK, int BV, int GS, int HP, int NL, bool MANY, bool RAGGED>
+template <int BK, int BV, int GS, int HP, int NL, bool MANY, bool SHARED>
 __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Plan<BK, BV, GS, HP, NL, MANY>::CTAS)
     decode_mma_kernel(const __grid_constant__ DecodeParams p) {
   using Pl = Plan<BK, BV, GS, HP, NL, MANY>;
@@ -402,12 +402,14 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     const int split = (int)(blockIdx.x - stream * (unsigned)p.ns_q);
     const int bh = (int)stream, b = (int)(stream / (unsigned)dm.Hkv);
     int n_q = p.n_q, r = p.r;
-    if constexpr (RAGGED) {
+    if constexpr (SHARED) {
       // the tokens of this sequence that exist; lengths may come from the preceding kernel
       if (!p.late_wait) grid_dependency_wait();
-      const int S = max(0, min(n_q + r, p.lengths[b]));
-      n_q = min(n_q, S);
-      r = S - n_q;
+      if (p.lengths != nullptr) {
+        const int S = max(0, min(n_q + r, p.lengths[b]));
+        n_q = min(n_q, S);
+        r = S - n_q;
+      }
       place_sm[7] = n_q;
     }
     const int nbt = (n_q + BT - 1) / BT;  // batches of the stream (the last one may be ragged)
@@ -509,7 +511,10 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
   if (tid < VH * D / 8) {
     const int v = tid / (D / 8), layer = v / HP, h = v % HP;
     uint4 x = make_uint4(0u, 0u, 0u, 0u);
-    if (h < G) x = reinterpret_cast<const uint4*>(LL[layer].q + ((size_t)place2.x * dm.Hq + place2.y * G + h) * D)[tid % (D / 8)];
+    if (h < G) {
+      const size_t row = SHARED ? shared_row(dm, p.each, place2.x, place2.y, h) : (size_t)place2.x * dm.Hq + place2.y * G + h;
+      x = reinterpret_cast<const uint4*>(LL[layer].q + row * D)[tid % (D / 8)];
+    }
     reinterpret_cast<uint4*>(q_sm)[tid] = x;
     const uint32_t sign = 0x7fff7fffu;  // both formats order like their bits without the sign
     uint32_t mx = __vmaxu2(__vmaxu2(x.x & sign, x.y & sign), __vmaxu2(x.z & sign, x.w & sign));
@@ -654,7 +659,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
   int last_k = 0, last_v = 0;  // rounds whose key codes, values were copied last
 #pragma unroll 1
   for (int r = 0; r < rounds; ++r) {
-    const int valid = min(TT, (RAGGED ? place2.w : p.n_q) - b0 * BT - (warp + W * r) * TT);  // < TT only in the stream's last round
+    const int valid = min(TT, (SHARED ? place2.w : p.n_q) - b0 * BT - (warp + W * r) * TT);  // < TT only in the stream's last round
     if (!__all_sync(0xffffffffu, mbar_wait(bar_k, r & 1, &dead_sm))) break;
 
     if (valid < TT) {  // what no token has reached may be anything: no scale, no zero-point
@@ -1320,9 +1325,10 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     for (int t = wrow0; t < wrow1; ++t) add(row((t + halves) % W, true));
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
-      if (RAGGED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
-      store_out(p, LL[layer], hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
-      if (NL == 1 && d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
+      if (SHARED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
+      const size_t to = SHARED ? shared_row(dm, p.each, b, hk, h) : hq;
+      store_out(p, LL[layer], to, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
+      if (NL == 1 && d == 0 && p.lse != nullptr) p.lse[to] = M + log2f(Ls);
     } else {
       const size_t at = ((size_t)layer * dm.B * dm.Hq + hq) * p.ns_q + split;
       *reinterpret_cast<float4*>(part_acc + at * D + d) = A;
@@ -1330,7 +1336,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     }
   }
   if (ns > 1)
-    ticket_merge<NL, RAGGED>(p, LL, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
+    ticket_merge<NL, SHARED>(p, LL, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
                         reinterpret_cast<float*>(smem));
 }
 
@@ -1353,9 +1359,9 @@ MmaShape shape_one() {
   return {Pl::WARPS, ready};
 }
 
-// The variant for sequences of their own lengths: its launches are fewer, and it is prepared with each.
+// The variant for many rows that read one cache: its launches are fewer, and it is prepared with each.
 template <int BK, int BV, int GS, int HP, int NL, bool MANY>
-cudaError_t launch_ragged_one(const DecodeParams& p, cudaStream_t st) {
+cudaError_t launch_shared_one(const DecodeParams& p, cudaStream_t st) {
   using Pl = Plan<BK, BV, GS, HP, NL, MANY>;
   auto kernel = decode_mma_kernel<BK, BV, GS, HP, NL, MANY, true>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Pl::TOTAL);
@@ -1385,11 +1391,15 @@ cudaError_t launch_decode_mma_t(const DecodeParams& p, cudaStream_t st) {
   return cudaErrorInvalidValue;
 }
 template <int HP>
-cudaError_t launch_decode_ragged_t(const DecodeParams& p, cudaStream_t st) {
+int decode_shared_warps_t(int g, int bk, int bv) {
+  return Plan<2, 2, 32, HP, 1, false>::WARPS;  // (of every variant)
+}
+template <int HP>
+cudaError_t launch_decode_shared_t(const DecodeParams& p, cudaStream_t st) {
   constexpr int NL = 1;
   constexpr bool MANY = false;
   const int bk = p.layer[0].L.bk, bv = p.layer[0].L.bv, g = p.dm.g;
-  XQ_DISPATCH(launch_ragged_one, p, st)
+  XQ_DISPATCH(launch_shared_one, p, st)
   return cudaErrorInvalidValue;
 }
 template <int HP, int NL, bool MANY>

@@ -223,8 +223,8 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, const DecodeLay
 // out = sum_s acc_s 2^(m_s-M) / sum_s l_s 2^(m_s-M).  No CTA ever waits for another.
 // What it takes is two trips to L2, one for all (m, l) and one for the partials: a warp that went through its share of
 // the heads one after the other, both trips for each, made it 2.3 us with four heads and 5.1 us with eight.
-// weights: G * (ns + 1) floats of shared memory.  RAGGED: a stream may have no token at all, its result is zero.
-template <bool RAGGED>
+// weights: G * (ns + 1) floats of shared memory.  SHARED: a stream may have no token at all, its result is zero.
+template <bool SHARED>
 __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const DecodeLayer& L, int ns, int hk, int b,
                                              const float* part_acc, const float* part_ml, unsigned* ticket, int* s_flag,
                                              float* weights) {
@@ -253,7 +253,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       M = x.x;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = lane < ns && !(RAGGED && x.x == -CUDART_INF_F) ? ex2(x.x - M) : 0.f;
+      const float f = lane < ns && !(SHARED && x.x == -CUDART_INF_F) ? ex2(x.x - M) : 0.f;
       Ls = x.y * f;
       if (lane < ns) w[lane] = f;
     } else {
@@ -262,7 +262,7 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       for (int s = lane; s < ns; s += 32) {
         const float2 x = ld_cg2(ml + 2 * s);
-        const float f = RAGGED && x.x == -CUDART_INF_F ? 0.f : ex2(x.x - M);
+        const float f = SHARED && x.x == -CUDART_INF_F ? 0.f : ex2(x.x - M);
         Ls = fmaf(x.y, f, Ls);
         w[s] = f;
       }
@@ -270,8 +270,8 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
     if (lane == 0) {
-      w[ns] = RAGGED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
-      if (p.lse != nullptr) p.lse[hq0 + h] = M + log2f(Ls);
+      w[ns] = SHARED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
+      if (p.lse != nullptr) p.lse[SHARED ? shared_row(dm, p.each, b, hk, h) : hq0 + h] = M + log2f(Ls);
     }
   }
   __syncthreads();
@@ -294,12 +294,12 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       }
     }
     const float inv = w[ns];
-    store_out(p, L, hq0 + h, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+    store_out(p, L, SHARED ? shared_row(dm, p.each, b, hk, h) : hq0 + h, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
   }
   if (threadIdx.x == 0) *ticket = 0u;  // ready for the next launch on this stream
 }
 
-template <int BK, int BV, int GS, int HP, int NT, bool RAGGED>
+template <int BK, int BV, int GS, int HP, int NT, bool SHARED>
 __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK, BV, GS, HP, NT>::CTAS)
     decode_mma64_kernel(const __grid_constant__ DecodeParams p) {
   using Pl = Plan<BK, BV, GS, HP, NT>;
@@ -331,12 +331,14 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
   const int hk = (int)(stream % (unsigned)dm.Hkv), b = (int)(stream / (unsigned)dm.Hkv);
   const int bh = b * dm.Hkv + hk;
   int n_q = p.n_q, r = p.r;
-  if constexpr (RAGGED) {
+  if constexpr (SHARED) {
     // the tokens of this sequence that exist; lengths may come from the preceding kernel
     if (!p.late_wait) grid_dependency_wait();
-    const int S = max(0, min(n_q + r, p.lengths[b]));
-    n_q = min(n_q, S);
-    r = S - n_q;
+    if (p.lengths != nullptr) {
+      const int S = max(0, min(n_q + r, p.lengths[b]));
+      n_q = min(n_q, S);
+      r = S - n_q;
+    }
   }
   const int nbt = (n_q + BT - 1) / BT;  // batches of the stream (the last one may be ragged)
   int b0, b1, wt0, wt1;
@@ -403,8 +405,9 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
   // ---- q ----
   for (int i = tid; i < HP * NT * D / 8; i += W * 32) {
     const bool real = i / (D / 8) < G;
-    const uint4* src = reinterpret_cast<const uint4*>(L.q + ((size_t)b * dm.Hq + hk * G) * D);
-    reinterpret_cast<uint4*>(q_sm)[i] = real ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+    const uint4* src = reinterpret_cast<const uint4*>(L.q + ((size_t)b * dm.Hq + hk * G) * D) + i;
+    if (SHARED && real) src = reinterpret_cast<const uint4*>(L.q + shared_row(dm, p.each, b, hk, i / (D / 8)) * D) + i % (D / 8);
+    reinterpret_cast<uint4*>(q_sm)[i] = real ? *src : make_uint4(0u, 0u, 0u, 0u);
   }
   __syncthreads();
   // exponents that put a head's largest |q| into [1, 2): each warp finds those of all heads; lane h keeps head h's
@@ -498,7 +501,7 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
   int last_k = 0, last_v = 0;  // number of the copy that each barrier was armed for last
 #pragma unroll 1
   for (int i = warp, it = 0; i < nb; i += W, ++it) {
-    const int valid = min(BT, (RAGGED ? n_q : p.n_q) - (b0 + i) * BT);  // < BT only in the stream's last batch
+    const int valid = min(BT, (SHARED ? n_q : p.n_q) - (b0 + i) * BT);  // < BT only in the stream's last batch
     if (!__all_sync(0xffffffffu, mbar_wait(bar_k, it & 1, &dead_sm))) break;
 
     // ---- keys: scales into the order of the operand slots (in place), the largest of them ----
@@ -997,16 +1000,17 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
     }
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
-      if (RAGGED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
-      store_out(p, L, hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
-      if (d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
+      if (SHARED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
+      const size_t to = SHARED ? shared_row(dm, p.each, b, hk, h) : hq;
+      store_out(p, L, to, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
+      if (d == 0 && p.lse != nullptr) p.lse[to] = M + log2f(Ls);
     } else {
       *reinterpret_cast<float4*>(part_acc + (hq * p.ns_q + split) * D + d) = A;
       if (d == 0) *reinterpret_cast<float2*>(part_ml + (hq * p.ns_q + split) * 2) = make_float2(M, Ls);
     }
   }
   if (ns > 1)
-    ticket_merge<RAGGED>(p, L, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
+    ticket_merge<SHARED>(p, L, ns, hk, b, part_acc, part_ml, p.tickets + (size_t)blockIdx.y * (dm.B * dm.Hkv) + bh, &s_flag,
                     reinterpret_cast<float*>(smem));
 }
 
@@ -1029,9 +1033,13 @@ MmaShape shape_one() {
   return {Pl::WARPS, ready};
 }
 
-// The variant for sequences of their own lengths: its launches are fewer, and it is prepared with each.
+// The variant for many rows that read one cache: its launches are fewer, and it is prepared with each.
 template <int BK, int BV, int GS, int HP, int NT>
-cudaError_t launch_ragged_one(const DecodeParams& p, cudaStream_t st) {
+int warps_one() {
+  return Plan<BK, BV, GS, HP, NT>::WARPS;
+}
+template <int BK, int BV, int GS, int HP, int NT>
+cudaError_t launch_shared_one(const DecodeParams& p, cudaStream_t st) {
   using Pl = Plan<BK, BV, GS, HP, NT>;
   auto kernel = decode_mma64_kernel<BK, BV, GS, HP, NT, true>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Pl::TOTAL);
@@ -1061,9 +1069,14 @@ cudaError_t launch_decode_mma64_t(const DecodeParams& p, cudaStream_t st) {
   return cudaErrorInvalidValue;
 }
 template <int HP, int NT>
-cudaError_t launch_decode_ragged64_t(const DecodeParams& p, cudaStream_t st) {
+int decode_shared64_warps_t(int g, int bk, int bv) {
+  XQ_DISPATCH(warps_one)
+  return 1;
+}
+template <int HP, int NT>
+cudaError_t launch_decode_shared64_t(const DecodeParams& p, cudaStream_t st) {
   const int bk = p.layer[0].L.bk, bv = p.layer[0].L.bv, g = p.dm.g;
-  XQ_DISPATCH(launch_ragged_one, p, st)
+  XQ_DISPATCH(launch_shared_one, p, st)
   return cudaErrorInvalidValue;
 }
 template <int HP, int NT>

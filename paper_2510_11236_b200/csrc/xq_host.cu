@@ -176,6 +176,8 @@ struct xq_cache {
   std::vector<uint8_t> repacked;  // per layer: codes or parameters it reads were written since its last decode
   MmaKernels mma_kernels[2][2];  // by (key bits - 1, value bits - 1)
   MmaPlan mma_plan[2][2];    // and the splits of the latest number of batches asked for; batches 0 = none yet
+  MmaPlan shared_plan;       // the same of calls whose rows read one cache, and what it was made for
+  int shared_key[4];
   // lists of xq_decode_step, n_layers long from the start: a step allocates nothing, and so cannot run out of host memory
   // (an exception) when some of its launches are under way
   std::vector<int> step_len, step_order, step_run;
@@ -223,7 +225,7 @@ bool uses_mma(const xq_cache* c) {
 #define XQ_MMA128(FN, ...) (dm.G == 1 ? FN<1, 1, false>(__VA_ARGS__) : dm.G == 2 ? FN<2, 1, false>(__VA_ARGS__) : dm.G <= 4 ? FN<4, 1, false>(__VA_ARGS__) : FN<8, 1, false>(__VA_ARGS__))
 #define XQ_MMA_MANY(FN, ...) (dm.G == 1 ? FN<1, 1, true>(__VA_ARGS__) : dm.G == 2 ? FN<2, 1, true>(__VA_ARGS__) : FN<4, 1, true>(__VA_ARGS__))
 #define XQ_MMA_PAIRS(FN, ...) (dm.G == 1 ? FN<1, 2, false>(__VA_ARGS__) : dm.G == 2 ? FN<2, 2, false>(__VA_ARGS__) : FN<4, 2, false>(__VA_ARGS__))
-#define XQ_MMA_RAGGED(FN, ...) (dm.G == 1 ? FN<1>(__VA_ARGS__) : dm.G == 2 ? FN<2>(__VA_ARGS__) : dm.G <= 4 ? FN<4>(__VA_ARGS__) : FN<8>(__VA_ARGS__))
+#define XQ_MMA_SHARED(FN, ...) (dm.G == 1 ? FN<1>(__VA_ARGS__) : dm.G == 2 ? FN<2>(__VA_ARGS__) : dm.G <= 4 ? FN<4>(__VA_ARGS__) : FN<8>(__VA_ARGS__))
 #define XQ_MMA64(FN, ...) (dm.G == 1 ? FN<1, 1>(__VA_ARGS__) : dm.G == 2 ? FN<2, 1>(__VA_ARGS__) : dm.G <= 4 ? FN<4, 1>(__VA_ARGS__) : FN<4, 2>(__VA_ARGS__))
 
 cudaError_t launch_decode_mma(const DecodeParams& p, cudaStream_t st) {
@@ -231,7 +233,7 @@ cudaError_t launch_decode_mma(const DecodeParams& p, cudaStream_t st) {
   if (p.paired && p.n_layers % 2) return cudaErrorInvalidValue;  // (the last one would have no CTA)
   if (p.paired) return XQ_MMA_PAIRS(launch_decode_mma_t, p, st);
   if (p.many) return XQ_MMA_MANY(launch_decode_mma_t, p, st);
-  if (p.lengths) return dm.D == 128 ? XQ_MMA_RAGGED(launch_decode_ragged_t, p, st) : XQ_MMA64(launch_decode_ragged64_t, p, st);
+  if (p.shared) return dm.D == 128 ? XQ_MMA_SHARED(launch_decode_shared_t, p, st) : XQ_MMA64(launch_decode_shared64_t, p, st);
   return dm.D == 128 ? XQ_MMA128(launch_decode_mma_t, p, st) : XQ_MMA64(launch_decode_mma64_t, p, st);
 }
 
@@ -296,11 +298,10 @@ DecodeTimes decode_times(const Dims& dm) {
 constexpr double ALONE_BOUND = 1.10, STEP_WEIGHT = 1.2;
 constexpr int WAVE_CTAS = 2;    // CTAs of a layer's own launch on an SM: the third place, where there is one, is the next launch's
 constexpr double MERGE = 0.03;  // us of a launch's end for each partial of a stream
-void plan_batches(const xq_cache* c, int warps, int batches, int splits, MmaPlan& out) {
-  const Dims& dm = c->plan.dm;
-  const long long streams = (long long)dm.B * dm.Hkv, slots = (long long)c->sm_count * WAVE_CTAS;
+void plan_batches(const Dims& dm, int sm_count, int n_layers, int warps, int batches, int splits, MmaPlan& out) {
+  const long long streams = (long long)dm.B * dm.Hkv, slots = (long long)sm_count * WAVE_CTAS;
   const DecodeTimes t = decode_times(dm);
-  const bool joint = c->cfg.n_layers >= MIN_JOINT_LAYERS;
+  const bool joint = n_layers >= MIN_JOINT_LAYERS;
   struct Candidate { int ns, deal; double alone, step, next; };
   Candidate all[2 * XQ_MAX_SPLITS];
   int n = 0;
@@ -318,7 +319,7 @@ void plan_batches(const xq_cache* c, int warps, int batches, int splits, MmaPlan
       const int per = ns > 1 && others > last ? others : last;
       // the last wave: a start and an end, and the rounds of a CTA, whose last one may leave warps without a batch
       auto wave = [&](long long ctas) {
-        long long resident = (ctas + c->sm_count - 1) / c->sm_count;
+        long long resident = (ctas + sm_count - 1) / sm_count;
         if (resident > WAVE_CTAS) resident = WAVE_CTAS;
         const int rounds = per / warps;
         double left = (double)batches / ns - rounds * warps;  // on average: the SM's CTAs share its rate
@@ -332,7 +333,7 @@ void plan_batches(const xq_cache* c, int warps, int batches, int splits, MmaPlan
         const long long last_wave = (ctas - 1) % slots + 1;
         return (double)((ctas - last_wave) / slots) * each + wave(last_wave);
       };
-      Candidate k{ns, deal, launch(streams * ns), joint ? launch(streams * ns * c->cfg.n_layers) / c->cfg.n_layers : 1.0,
+      Candidate k{ns, deal, launch(streams * ns), joint ? launch(streams * ns * n_layers) / n_layers : 1.0,
                   (dm.G > 4 ? 5.5 : 2.5) + (double)(streams * ns) / slots * (each + (takes_pairs(dm) ? t.cta : 0.0))};
       if (k.alone < t.floor) k.alone = t.floor;
       if (n == 0 || k.alone < alone_min) alone_min = k.alone;
@@ -356,7 +357,8 @@ void plan_batches(const xq_cache* c, int warps, int batches, int splits, MmaPlan
 // The plan of a number of batches is kept: making it costs the host about 10 us at 32k.
 const MmaPlan& batches_plan(const xq_cache* c, int l, int batches) {
   MmaPlan& plan = const_cast<xq_cache*>(c)->mma_plan[layer_bits(l, c->cfg.kq) - 1][layer_bits(l, c->cfg.vq) - 1];
-  if (plan.batches != batches) plan_batches(c, mma_kernels(c, l).warps, batches, c->cfg.n_splits < batches ? c->cfg.n_splits : batches, plan);
+  if (plan.batches != batches)
+    plan_batches(c->plan.dm, c->sm_count, c->cfg.n_layers, mma_kernels(c, l).warps, batches, c->cfg.n_splits < batches ? c->cfg.n_splits : batches, plan);
   return plan;
 }
 
@@ -497,6 +499,8 @@ int prepare_decode(const xq_cache* c, int layer, const void* q, void* out, int o
   p.late_wait = 0;
   p.f16 = c->cfg.io_dtype == XQ_F16;
   p.lse = nullptr;
+  p.shared = 0;
+  p.each = 1;
   p.lengths = nullptr;
   return XQ_OK;
 }
@@ -811,6 +815,8 @@ int xq_create(const xq_config* cfg, void* dev_workspace, size_t bytes, xq_cache*
   c->static_base = nullptr;
   memset(c->mma_kernels, 0, sizeof(c->mma_kernels));
   memset(c->mma_plan, 0, sizeof(c->mma_plan));
+  memset(&c->shared_plan, 0, sizeof(c->shared_plan));
+  memset(c->shared_key, 0, sizeof(c->shared_key));
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) == cudaSuccess &&
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && sms > 0) {
@@ -1131,24 +1137,60 @@ int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_a
   return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
 }
 
-// Query tokens of each sequence against a whole cache in decode launches, one for each of the T tokens, chained (where the rows
-// of a kv head are few: see rows_one_by_one).  kv: the cache that is read; c: the handle whose scratch and status word the call
-// uses.  lse: [T,B,Hq] or null.
-int launch_rows_decode(xq_cache* c, xq_cache* kv, int layer, int T, const int* lengths, const void* q, void* out, int out_f32,
-                       float* lse, cudaStream_t st) {
-  const Dims& dm = kv->plan.dm;
-  const size_t rows = (size_t)dm.B * dm.Hq;
+// Few rows of a kv head go to the decode kernels, a launch for each of the T tokens of a sequence, chained.
+struct SharedDecode {
+  Dims dm;  // of the decode launches: G counts the heads of all sequences that share a cache
+  MmaPlan plan;
+};
+// The launches' splits (kept in the handle: making them costs the host about 10 us at 32k); false: not for these kernels.
+bool shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, SharedDecode& out) {
+  out.dm = kv->plan.dm;
+  out.dm.G = r.each * kv->plan.dm.G;
+  out.dm.Hq = out.dm.Hkv * out.dm.G;
+  const Dims& dm = out.dm;
+  if (dm.G > 8 || !uses_mma(kv) || c->cfg.kernel == XQ_KERNEL_GENERIC) return false;
+  const int bk = layer_bits(layer, kv->cfg.kq), bv = layer_bits(layer, kv->cfg.vq);
+  const int warps = dm.D == 128 ? XQ_MMA_SHARED(decode_shared_warps_t, dm.g, bk, bv) : XQ_MMA64(decode_shared64_warps_t, dm.g, bk, bv);
+  const int S = kv->seq[layer], window = residual_count(S, dm.R), batches = (S - window + XQ_BATCH - 1) / XQ_BATCH;
+  if (batches == 0) {  // the window alone, as in plan_splits
+    const int tiles = (window + 15) / 16, most = std::max(1, c->sm_count * WAVE_CTAS / (dm.B * dm.Hkv));
+    out.plan = {0, std::max(1, std::min({(tiles + warps - 1) / warps, most, tiles})), 1, decode_times(dm).launch, 2.5};
+    return true;
+  }
+  const int key[4] = {dm.B * dm.Hkv, dm.G, warps, dm.D};
+  if (c->shared_plan.batches != batches || memcmp(key, c->shared_key, sizeof(key)) != 0) {
+    plan_batches(dm, c->sm_count, 1, warps, batches, 0, c->shared_plan);
+    memcpy(c->shared_key, key, sizeof(key));
+  }
+  out.plan = c->shared_plan;
+  return true;
+}
+
+// kv: the cache that is read; c: the handle whose scratch and status word the call uses.  lse: [T,Bq,Hq] or null.
+int launch_shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, const SharedDecode& d, int T, const int* lengths,
+                         const void* q, void* out, int out_f32, float* lse, cudaStream_t st) {
+  const size_t rows = (size_t)(r.rows / T);
+  const int S = kv->seq[layer];
+  DecodeParams p;
+  p.dm = d.dm;
+  p.n_layers = 1;
+  p.paired = p.many = 0;
+  p.r = residual_count(S, d.dm.R);
+  p.n_q = S - p.r;
+  p.ns_q = d.plan.ns;
+  p.ns_w = 0;
+  p.deal = d.plan.deal;
+  p.scale = c->scale;
+  p.out_f32 = out_f32;
+  p.f16 = c->cfg.io_dtype == XQ_F16;
+  p.shared = 1;
+  p.each = r.each;
+  p.lengths = lengths;
   for (int j = 0; j < T; ++j) {
-    DecodeParams p;
-    bool use_mma = false;
-    int rc = prepare_decode(kv, layer, (const uint8_t*)q + j * rows * dm.D * 2, (uint8_t*)out + j * rows * dm.D * (out_f32 ? 4 : 2), out_f32,
-                            nullptr, nullptr, kv->seq[layer], p, use_mma);
-    if (rc != XQ_OK) return rc;
-    p.scale = c->scale;
+    p.layer[0] = {layer_ptrs(kv, layer), (const uint16_t*)q + j * rows * d.dm.D, (uint8_t*)out + j * rows * d.dm.D * (out_f32 ? 4 : 2), nullptr, nullptr};
     p.lse = lse ? lse + j * rows : nullptr;
-    p.lengths = lengths;
-    if (j > 0) p.early_fetch = p.late_wait = 1;  // what this launch reads was complete when the first one had waited
-    rc = launch_decode(c, p, use_mma, workspace_scratch(c), st);
+    p.early_fetch = p.late_wait = j > 0;  // what this launch reads was complete when the first one had waited
+    const int rc = launch_decode(c, p, true, workspace_scratch(c), st);
     if (rc != XQ_OK) {
       c->tickets_clean = false;
       return rc;
@@ -1157,15 +1199,10 @@ int launch_rows_decode(xq_cache* c, xq_cache* kv, int layer, int T, const int* l
   return XQ_OK;
 }
 
-// Whether T query tokens of each sequence take less time as decode launches than as one rows call (one sequence of queries for
-// each of the cache, heads that the tensor-core decode kernels take).  Modelled times in us: decode as plan_batches has them;
-// rows as rows_splits does.
-bool rows_one_by_one(const xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, int T, int ns) {
-  const Dims& dm = kv->plan.dm;
-  if (r.each != 1 || T > 16 || !uses_mma(kv) || c->cfg.kernel == XQ_KERNEL_GENERIC) return false;
-  const int S = kv->seq[layer], batches = (S - residual_count(S, dm.R) + XQ_BATCH - 1) / XQ_BATCH;
-  const MmaPlan window{0, 0, 1, decode_times(dm).launch, 2.5}, &plan = batches > 0 ? batches_plan(kv, layer, batches) : window;
-  return plan.alone + (T - 1) * plan.next < rows_time(kv, r, S, ns);
+// Whether T decode launches take less time than one rows call: modelled times in us, decode as plan_batches has them, rows as
+// rows_splits does.
+bool rows_one_by_one(const xq_cache* kv, int layer, const RowsPlan& r, const SharedDecode& d, int T, int ns) {
+  return T <= 16 && d.plan.alone + (T - 1) * d.plan.next < rows_time(kv, r, kv->seq[layer], ns);
 }
 
 // Whether the handle's device is the current one (a handle made without a device has none).
@@ -1214,9 +1251,10 @@ int prefix_impl(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* o
     rc = chunk_impl(c, layer, q, own, T, 1, stream, lse);
     if (rc != XQ_OK) return rc;
   }
-  if (rows_one_by_one(c, prefix, layer, plan, T, ns)) {
-    if (S == 0) return launch_rows_decode(c, prefix, layer, T, nullptr, q, out, out_f32, nullptr, st);
-    rc = launch_rows_decode(c, prefix, layer, T, nullptr, q, acc, 1, ml, st);
+  SharedDecode d;
+  if (shared_decode(c, prefix, layer, plan, d) && rows_one_by_one(prefix, layer, plan, d, T, ns)) {
+    if (S == 0) return launch_shared_decode(c, prefix, layer, plan, d, T, nullptr, q, out, out_f32, nullptr, st);
+    rc = launch_shared_decode(c, prefix, layer, plan, d, T, nullptr, q, acc, 1, ml, st);
     if (rc != XQ_OK) return rc;
     return launch_rows_join(c, plan, 1, acc, nullptr, ml, own, lse, out, out_f32, st);
   }
@@ -1248,7 +1286,9 @@ int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const in
   if (rc != XQ_OK) return rc;
   uint8_t* w = (uint8_t*)workspace;
   float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml);
-  if (rows_one_by_one(c, c, layer, plan, T, ns)) return launch_rows_decode(c, c, layer, T, lengths, q, out, out_f32, nullptr, st);
+  SharedDecode d;
+  if (shared_decode(c, c, layer, plan, d) && rows_one_by_one(c, layer, plan, d, T, ns))
+    return launch_shared_decode(c, c, layer, plan, d, T, lengths, q, out, out_f32, nullptr, st);
   const bool direct = ns == 1 && c->cfg.kernel != XQ_KERNEL_GENERIC;
   rc = launch_rows(c, c, layer, plan, T, ns, lengths, q, out, out_f32, direct ? nullptr : acc, ml, st);
   if (rc != XQ_OK || direct) return rc;

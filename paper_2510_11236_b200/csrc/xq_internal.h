@@ -115,7 +115,11 @@ struct DecodeParams {
   // [B,Hq] or null (launches of one layer): log2 of each result's softmax denominator, sum 2^(logit / ln 2), for callers
   // that join the result with another one over other tokens
   float* lse;
-  const int* lengths;  // [B] or null: the tokens of each sequence that exist (the variants of the tensor-core kernels for it)
+  // The variants of the tensor-core kernels for many rows that read one cache (prefix and cross attention), one layer:
+  int shared;          // 1: take them.  A sequence of the cache then serves `each` sequences of the queries, and dm.G is each
+                       // times the heads of a kv head: "head" v of a kv head is head v % (G / each) of the sequence v / (G / each)
+  int each;
+  const int* lengths;  // [B] or null: the tokens of each sequence that exist
   DecodeLayer layer[DECODE_MAX_LAYERS];
 };
 
@@ -155,6 +159,11 @@ struct MergeParams {
 // of the cache serves the sequences u * each .. u * each + each - 1 of the queries.  A row is (token j, one of these
 // sequences i, head h of a kv head): row (j * each + i) * G + h of its stream, and row (j * Bq + u * each + i) * Hq + hk * G
 // + h of the call.
+// Row of the call's q and result for "head" v of kv head hk and sequence u of the cache (DecodeParams::shared).
+__host__ __device__ inline size_t shared_row(const Dims& dm, int each, int u, int hk, int v) {
+  const int heads = dm.G / each;
+  return ((size_t)u * each + v / heads) * (dm.Hkv * heads) + hk * heads + v % heads;
+}
 struct RowsParams {
   Dims dm;             // of the cache (B: its sequences)
   LayerPtrs L;
@@ -257,11 +266,15 @@ template <int HP, int NT>
 cudaError_t launch_decode_mma64_t(const DecodeParams& p, cudaStream_t st);
 template <int HP, int NT>
 MmaShape decode_mma64_shape_t(int g, int bk, int bv);
-// the same, of one layer, for sequences of their own lengths
+// the same for many rows that read one cache (DecodeParams::shared), and the warps of their CTAs
 template <int HP>
-cudaError_t launch_decode_ragged_t(const DecodeParams& p, cudaStream_t st);
+cudaError_t launch_decode_shared_t(const DecodeParams& p, cudaStream_t st);
 template <int HP, int NT>
-cudaError_t launch_decode_ragged64_t(const DecodeParams& p, cudaStream_t st);
+cudaError_t launch_decode_shared64_t(const DecodeParams& p, cudaStream_t st);
+template <int HP>
+int decode_shared_warps_t(int g, int bk, int bv);
+template <int HP, int NT>
+int decode_shared64_warps_t(int g, int bk, int bv);
 template <int D>
 cudaError_t launch_chunk_t(const ChunkParams& p, cudaStream_t st);
 cudaError_t launch_merge(const MergeParams& p, cudaStream_t st);

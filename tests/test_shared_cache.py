@@ -269,6 +269,15 @@ def test_prefix_of_its_own(shape, S, T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Sp,S,T", [(700, 33, 1), (50, 9, 3), (129, 0, 1)])
+@pytest.mark.parametrize("shape,P,each", [(SHAPES[2], 1, 8), (SHAPES[2], 2, 3), (SHAPES[0], 2, 2), (SHAPES[3], 3, 2), (SHAPES[4], 1, 2),
+                                          ((64, 2, 2, 32, 32, 0, 2, False), 2, 4)])
+def test_prefix_few_rows(shape, P, each, Sp, S, T):
+    # at most eight rows of a kv head: the decode kernels, several sequences' heads on one cache
+    _prefix_case(shape, xq.XQ_KERNEL_AUTO, P, each, Sp, S, T)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[6]])
 def test_prefix_behind_long_tails(shape):
     # the sequences' own tokens in several splits: one token (decode kernels) and twenty (chunk kernel)
