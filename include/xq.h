@@ -220,8 +220,10 @@ int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, in
  * one handle c are ordered by the caller, as all calls of a handle are.  A call captured into a graph keeps the
  * lengths it was captured with.
  * Precision: codes, scales and zero-points enter the matrix products exactly, q as half precision relative to
- * the row's largest element, the softmax numerators are rounded to half precision (2^-12 of each; their sum is
- * that of the rounded ones), sums are fp32.  XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.
+ * the row's largest element (exactly, if it is half precision), the softmax numerators rounded to half precision
+ * where io_dtype is bfloat16 (at most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits
+ * where it is half precision; sums are fp32.  Up to eight rows of a kv head: as xq_decode_attention.
+ * XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.
  * The _f32 variant writes float results (tests).  Errors as xq_attention_chunk; XQ_ERR_ARG also: both layers
  * empty, 0 < S < n_q_tokens, current device not the handles'; XQ_ERR_CAPACITY: workspace too small. */
 size_t xq_prefix_workspace_bytes(const xq_cache* c, const xq_cache* prefix, int n_q_tokens);

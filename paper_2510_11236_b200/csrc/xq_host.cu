@@ -1108,7 +1108,8 @@ int launch_rows(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, i
   {
     Timer t(c, st, 0);
     if (c->cfg.kernel == XQ_KERNEL_GENERIC) e = launch_rows_generic(p, st);
-    else e = dm.D == 128 ? launch_rows_t<128>(p, st) : launch_rows_t<64>(p, st);
+    else if (p.f16) e = dm.D == 128 ? launch_rows_t<128, true>(p, st) : launch_rows_t<64, true>(p, st);
+    else e = dm.D == 128 ? launch_rows_t<128, false>(p, st) : launch_rows_t<64, false>(p, st);
   }
   c->launches++;
   return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);

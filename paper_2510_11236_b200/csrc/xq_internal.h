@@ -278,7 +278,7 @@ int decode_shared64_warps_t(int g, int bk, int bv);
 template <int D>
 cudaError_t launch_chunk_t(const ChunkParams& p, cudaStream_t st);
 cudaError_t launch_merge(const MergeParams& p, cudaStream_t st);
-template <int D>
+template <int D, bool F16>
 cudaError_t launch_rows_t(const RowsParams& p, cudaStream_t st);
 cudaError_t launch_rows_generic(const RowsParams& p, cudaStream_t st);
 cudaError_t launch_join(const JoinParams& p, cudaStream_t st);

@@ -6,14 +6,20 @@
 // 2 s, is a half-precision number when s is (1-bit codes: s c + z).  The rest does not depend on the token (keys: within a
 // group of tokens) or on the channel (values: within a group of channels), so it is a few more rows of the same operand:
 //
-//   S = Q [s (c - 1) | z, s of the token groups]                 128 + 16 columns, fp32
-//   O += P [s (c - 1) | z, s of the channel groups | 1]          head_dim + 16 columns, fp32; the last one sums P
+//   S = Q [s (c - 1) | z, s of the token groups]                    128 + 16 columns, fp32
+//   O += P [s (c - o) | z, o s of the channel groups | 1]           head_dim + 16 columns, fp32; the last one sums P
 //
-// Q: half precision, scaled by a power of two for each row (exact for bfloat16 down to 2^-16 of the row's largest element);
-// P: the softmax numerators times 2^R_PEXP, rounded to half precision (2^-12 of each on average; the result is divided by the
-// sum of the rounded ones), the one rounding of operands here.  Both are A operands in tensor memory.  Against pairs hi + lo of
-// codes and numerators, as the chunk kernel has them, that is 608 in place of 1280 cycles of the tensor pipe a tile, and half
-// the expansion.
+// o is 1 for even tokens, 2 for odd ones (1-bit values: 0 and 1).  Every addition of the tensor core to O drops what lies below
+// the sum's last digit, always in one direction, and a sum over P of terms with a mean is a multiple of the result where that
+// averages many tokens: with one o for all the codes' part has one, and z and o s each do.  So half precision takes z + o s,
+// which then has none, as two rows hi + lo.  16 tokens at 40000, half precision, error in the result's norm, whose own rounding is
+// 2.07e-4: 2.61e-4 with o = 1, z and s; 2.45e-4 with hi + lo alone; 2.07e-4 with both.
+//
+// Q: half precision, scaled by a power of two for each row (exact for bfloat16 down to 2^-16 of the row's largest element).
+// P: the softmax numerators times 2^R_PEXP, in half precision, rounded for bfloat16 results (2e-4 of the result's norm, an eighth
+// of the result's own rounding; divided by the sum of the rounded P), as pairs hi + lo, a product each, for half-precision ones.
+// Q and P are A operands in tensor memory.  Against pairs of codes and numerators, as the chunk kernel has them, that is 576
+// (half precision: 864) in place of 1280 cycles of the tensor pipe for 64 tokens, and half the expansion.
 //
 // Tokens go in batches of 128, two tiles each, with two S.  Four groups of four softmax warps (thread = row = lane of tensor
 // memory) take the tiles in turn: a warp's steps are short and wait for one another, so it takes several to fill the SM.  The
@@ -109,7 +115,9 @@ struct RowsLayout {
   static constexpr int KN = RB + 16, VN = D + 16;      // rows of the operands: tokens and 16 more, channels and 16 more
   // an operand: blocks of 128-byte rows (64 channels of the keys, 64 tokens of the values)
   static constexpr int KBLOCK = KN * 128, KBYTES = D / 64 * KBLOCK, VBLOCK = VN * 128, VBYTES = RB / 64 * VBLOCK;
-  static constexpr int ONES = D + 8;                   // the operand row, and column of O, that sums P
+  // rows of the value operand, and columns of O, behind the channels: z of the channel groups; s, which only the expanding
+  // warps read; ones, which sum P; o s (half precision: the sum of z and o s, rounded, and what the rounding left off)
+  static constexpr int ZERO = D, SCALE = D + NG, ONES = D + 8, REST = D + 9;
   // a raw stage: key codes, key parameters, value codes, value parameters of a batch
   static constexpr int RAW_KM = RB * KROW, RAW_VC = RAW_KM + RB / GS * 4 * D, RAW_VM = RAW_VC + 16 * D * BV;
   static constexpr int RAW = RAW_VM + RB * 4 * NG;
@@ -121,16 +129,21 @@ struct RowsLayout {
   static_assert(COL_S + 2 * KN <= 512, "tensor memory");
 };
 
+// First column of the numerators of tokens 16 ks .. of a tile: in the place of their S, 32 tokens in 16 columns, half precision
+// rests 16 columns on
+__host__ __device__ constexpr uint32_t p_col(int ks) { return 32 * (ks >> 1) + 8 * (ks & 1); }
+
 // The byte of 16-byte piece `piece` of an operand row, from the operand's start
 __device__ __forceinline__ uint32_t piece_at(int row, int piece) { return (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4)); }
 
-// Sixteen codes, four fields (at bits 0, BITS, 2 BITS, 3 BITS of every byte of w) of four bytes each, times the scales of
-// their pairs.  A field becomes a half-precision number beside an exponent whose last places it takes: 2^(10 - BITS j) + c.
-template <int BITS>
+// Sixteen codes, four fields (at bits 0, BITS, 2 BITS, 3 BITS of every byte of w) of four bytes each, less OFFSET (the second
+// and the fourth of a field's bytes: less ODD), times the scales of their pairs.  A field becomes a half-precision number
+// beside an exponent whose last places it takes: 2^(10 - BITS j) + c.
+template <int BITS, int OFFSET>
 __device__ __forceinline__ uint32_t code_times(uint32_t w, int j, uint32_t s) {
   const uint32_t field = (BITS == 2 ? 0x00030003u : 0x00010001u) << (BITS * j);
-  const uint32_t base = 0x64006400u - 0x04000400u * (BITS * j);                      // 2^(10 - BITS j)
-  const uint32_t less = (base | 0x80008000u) + (BITS == 2 ? 0x00010001u << (2 * j) : 0u);  // and one more for two bits
+  const uint32_t base = 0x64006400u - 0x04000400u * (BITS * j);                        // 2^(10 - BITS j)
+  const uint32_t less = (base | 0x80008000u) + OFFSET * (0x00010001u << (BITS * j));   // and OFFSET more
   return hmul2(hadd2((w & field) | base, less), s);
 }
 template <int OFF>
@@ -143,11 +156,11 @@ __device__ __forceinline__ uint32_t lds32_at(uint32_t a) {
   asm volatile("ld.shared.u32 %0, [%1 + %2];\n" : "=r"(v) : "r"(a), "n"(OFF) : "memory");
   return v;
 }
-template <int BITS, int OFF>
+template <int BITS, int OFFSET, int ODD, int OFF>
 __device__ __forceinline__ void expand16(uint32_t w, const uint4& s0, const uint4& s1, uint32_t dst0, uint32_t dst1) {
   const uint32_t y = w >> 8;
-  sts128_at<OFF>(dst0, code_times<BITS>(w, 0, s0.x), code_times<BITS>(y, 0, s0.y), code_times<BITS>(w, 1, s0.z), code_times<BITS>(y, 1, s0.w));
-  sts128_at<OFF>(dst1, code_times<BITS>(w, 2, s1.x), code_times<BITS>(y, 2, s1.y), code_times<BITS>(w, 3, s1.z), code_times<BITS>(y, 3, s1.w));
+  sts128_at<OFF>(dst0, code_times<BITS, OFFSET>(w, 0, s0.x), code_times<BITS, ODD>(y, 0, s0.y), code_times<BITS, OFFSET>(w, 1, s0.z), code_times<BITS, ODD>(y, 1, s0.w));
+  sts128_at<OFF>(dst1, code_times<BITS, OFFSET>(w, 2, s1.x), code_times<BITS, ODD>(y, 2, s1.y), code_times<BITS, OFFSET>(w, 3, s1.z), code_times<BITS, ODD>(y, 3, s1.w));
 }
 // N rows of them, eight rows apart (1024 bytes of the operand), packed words STRIDE bytes apart; shift: of 1-bit codes' words
 template <int N, int STRIDE, int K = 0>
@@ -157,11 +170,11 @@ __device__ __forceinline__ void load_codes(uint32_t src, uint32_t (&w)[N]) {
     load_codes<N, STRIDE, K + 1>(src, w);
   }
 }
-template <int BITS, int N, int K = 0>
+template <int BITS, int OFFSET, int ODD, int N, int K = 0>
 __device__ __forceinline__ void expand_rows(const uint32_t (&w)[N], int shift, const uint4& s0, const uint4& s1, uint32_t dst0, uint32_t dst1) {
   if constexpr (K < N) {
-    expand16<BITS, 1024 * K>(BITS == 2 ? w[K] : w[K] >> shift, s0, s1, dst0, dst1);
-    expand_rows<BITS, N, K + 1>(w, shift, s0, s1, dst0, dst1);
+    expand16<BITS, OFFSET, ODD, 1024 * K>(BITS == 2 ? w[K] : w[K] >> shift, s0, s1, dst0, dst1);
+    expand_rows<BITS, OFFSET, ODD, N, K + 1>(w, shift, s0, s1, dst0, dst1);
   }
 }
 // Eight of them where a scale is too large to be doubled: c s + z, rounded (the operand's extra rows are then zero).  w:
@@ -184,8 +197,9 @@ __device__ __forceinline__ void restore8(uint32_t w, S s_at, Z z_at, uint32_t ds
 }
 
 // eight 16-bit numbers times f, as half precision in the operands' order: elements (0, 2), (1, 3), (4, 6), (5, 7)
-__device__ __forceinline__ uint4 reorder8(const uint4& v, float f, int f16) {
-  if (f16) return make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
+template <bool F16>
+__device__ __forceinline__ uint4 reorder8(const uint4& v, float f) {
+  if (F16) return make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
   auto lo = [&](uint32_t x) { return __uint_as_float(x << 16) * f; };
   auto hi = [&](uint32_t x) { return __uint_as_float(x & 0xffff0000u) * f; };
   return make_uint4(pack_io2<true>(lo(v.x), lo(v.y)), pack_io2<true>(hi(v.x), hi(v.y)), pack_io2<true>(lo(v.z), lo(v.w)), pack_io2<true>(hi(v.z), hi(v.w)));
@@ -201,7 +215,7 @@ __device__ __forceinline__ int window_exponent(float mx) {
   return (mx >= 0.0625f && mx < 32768.f) || !(mx > 0.f) ? 0 : 14 - exponent_of(mx);
 }
 
-template <int D, int BK, int BV, int GS>
+template <int D, int BK, int BV, int GS, bool F16>
 __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constant__ RowsParams p) {
   using Ly = RowsLayout<D, BK, BV, GS>;
   constexpr int NG = Ly::NG;
@@ -296,7 +310,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     uint32_t x = 0u;
 #pragma unroll
     for (int k = 0; k < R_EXPAND; ++k) x = max(x, m[k]);
-    return p.f16 ? 0 : window_exponent(bf16_top(x));
+    return F16 ? 0 : window_exponent(bf16_top(x));
   };
 
   // a batch's packed data into its raw stage
@@ -358,8 +372,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           tc_fence_after();
           if (elect_one()) {
             const uint64_t v = rows_desc(smu + Ly::OFF_V + b * Ly::VBYTES + g * Ly::VBLOCK);
+            const uint32_t P = dS + g * RT;
+            bool sum = i > 2 || g > 0;
+            if constexpr (F16) {  // the rests first: a sum drops what lies below its own last digit
 #pragma unroll
-            for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, dS + g * RT + 8 * ks, v + 2 * ks, IDV, i > 2 || g > 0 || ks > 0);
+              for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, P + p_col(ks) + 16, v + 2 * ks, IDV, sum || ks > 0);
+              sum = true;
+            }
+#pragma unroll
+            for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, P + p_col(ks), v + 2 * ks, IDV, sum || ks > 0);
             rows_commit(bar_o + 16 * b + 8 * g);
             if (g == 1) rows_commit(bar_vfree + 8 * b);
           }
@@ -417,7 +438,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     constexpr int PARTS = D / 64, STEPS = D / 32;
     const int kb = D == 128 ? ew & 1 : 0, slot0 = D == 128 ? ew & 2 : ew;
     const int v_c0 = ew * (D / 4), vg = v_c0 / GS;
-    const int rz = keys ? RB + 2 * slot0 : D + vg, rs = keys ? rz + 1 : rz + NG;  // operand rows of the zero-points and of the scales
+    const int rz = keys ? RB + 2 * slot0 : Ly::ZERO + vg, rs = keys ? rz + 1 : Ly::SCALE + vg;  // operand rows of the zero-points and of the scales
     const int row = keys ? 32 * slot0 + sub : v_c0 + sub;
     const int shift = ((keys ? BK : BV) == 2 ? 0 : 4) * (o & 1);
     constexpr int PERK = 32 / BK, CB = Ly::KROW < 16 ? Ly::KROW : 16;
@@ -429,6 +450,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     const uint32_t op_off = keys ? kb * Ly::KBLOCK : Ly::OFF_V;
     const int at = (lane & ~3) | ((lane & 1) << 1) | ((lane >> 1) & 1);  // place of channel `lane`: elements of four 0, 2, 1, 3
     const uint32_t params_off = keys ? piece_at(rz, at >> 3) + 2 * (at & 7) : piece_at(lane & 2 ? rz : rs, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;
+    const uint32_t rest_off = piece_at(Ly::REST + vg, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;  // values
     const uint32_t row_off = piece_at(row, 2 * o), scales_off = piece_at(rs, 2 * o);
     static_assert(PARTS <= 2 && RB % 8 == 0, "rows rz + 2 x: bit 1 of rz is clear where x can be 1");
     if (!keys && ew < 2 && lane < 8) {  // the row that sums the numerators
@@ -487,7 +509,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
             load_codes<4, 8 * CB>(src, codes);
             const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
-            expand_rows<BK, 4>(codes, shift, s0, s1, d0, d1);
+            expand_rows<BK, BK - 1, BK - 1, 4>(codes, shift, s0, s1, d0, d1);
           } else {
             const uint32_t group = raw + Ly::RAW_KM + (slot0 + x) * 32 / GS * (4 * D);
 #pragma unroll 1
@@ -501,7 +523,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       } else if (packed) {
         const int valid = n_q - (t_lo + i) * RB;  // tokens of the batch that exist
         // Parameters of tokens lane, lane + 32, + 64, + 96, (scale, zero-point); none of tokens that do not exist.  A word of the
-        // operand's rows has tokens (t, t + 2): one of the two lanes writes the scales, the other the zero-points.
+        // operand's rows has tokens (t, t + 2): one of the two lanes writes s and o s, the other z.
         uint32_t sz[4], large = 0u;  // bit x: of half x
 #pragma unroll
         for (int k = 0; k < 4; ++k) sz[k] = lds16(raw + meta_off + k * (128 * NG)) | lds16(raw + meta_off + k * (128 * NG) + 2 * NG) << 16;
@@ -514,9 +536,19 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           if (BV == 2 && __any_sync(0xffffffffu, (sz[2 * x] & 0xffffu) > MAX_DOUBLED || (sz[2 * x + 1] & 0xffffu) > MAX_DOUBLED)) large |= 1u << x;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2);
-          const uint32_t w = lane & 2 ? __byte_perm(other, sz[k], 0x7632) : __byte_perm(sz[k], other, 0x5410);
-          sts32((dst + params_off + (k >> 1) * Ly::VBLOCK) ^ (64u * (k & 1)), (large >> (k >> 1)) & 1u ? 0u : w);
+          const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2), first = lane & 2 ? other : sz[k], second = lane & 2 ? sz[k] : other;
+          uint32_t s2 = __byte_perm(first, second, 0x5410), z2 = __byte_perm(first, second, 0x7632);
+          if ((large >> (k >> 1)) & 1u) s2 = z2 = 0u;
+          const uint32_t to = (dst + params_off + (k >> 1) * Ly::VBLOCK) ^ (64u * (k & 1));
+          uint32_t os = BV == 2 ? (lane & 1 ? hadd2(s2, s2) : s2) : (lane & 1 ? s2 : 0u);
+          if constexpr (F16) {  // z and o s as the rounding of their sum and what it left off (D. E. Knuth's two-sum: exact)
+            constexpr uint32_t minus = 0x80008000u;
+            const uint32_t sum = hadd2(z2, os), t = hadd2(sum, z2 ^ minus);
+            os = hadd2(hadd2(z2, hadd2(t, sum ^ minus)), hadd2(os, t ^ minus));
+            z2 = sum;
+          }
+          sts32(to, lane & 2 ? z2 : s2);
+          if (!(lane & 2)) sts32((dst + rest_off + (k >> 1) * Ly::VBLOCK) ^ (64u * (k & 1)), os);
         }
         __syncwarp();
 #pragma unroll 1
@@ -527,7 +559,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             uint32_t codes[STEPS];
             load_codes<STEPS, 128>(src, codes);
             const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
-            expand_rows<BV, STEPS>(codes, shift, s0, s1, d0, d1);
+            expand_rows<BV, BV - 1, BV, STEPS>(codes, shift, s0, s1, d0, d1);
           } else {
             // (a token that does not exist stands for the last one that does: its numerator is zero)
 #pragma unroll 1
@@ -544,7 +576,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         const uint4* rows = reinterpret_cast<const uint4*>((keys ? p.L.win_k : p.L.win_v) + ((size_t)bh * dm.R + w0) * D);
         const uint32_t bar_unit = (keys ? bar_kunit : bar_vunit) + 8 * slot_w;
         float f = 1.f;
-        if (!p.f16) {
+        if (!F16) {
           uint32_t m = 0u;
 #pragma unroll 4
           for (int x = ew * 32 + lane; x < n_w * (D / 8); x += 128) m = top_of(m, rows[x]);
@@ -552,7 +584,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           if (lane == 0) unit_sm[slot_w][keys ? 0 : 1][ew] = m;
         }
         if (lane == 0) mbar_arrive(bar_unit);
-        if (!p.f16) {
+        if (!F16) {
           if (!warp_wait(bar_unit, ((i - n_pk) / R_UNITS) & 1, &dead_sm)) break;
           f = pow2i(batch_exponent(i, keys ? 0 : 1));
         }
@@ -562,15 +594,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
 #pragma unroll 4
           for (int x = ew * 32 + lane; x < RB * (D / 8); x += 128) {
             const int y = x / (D / 8), c = x % (D / 8);
-            const uint4 v = reorder8(y < n_w ? rows[x] : make_uint4(0u, 0u, 0u, 0u), f, p.f16);
+            const uint4 v = reorder8<F16>(y < n_w ? rows[x] : make_uint4(0u, 0u, 0u, 0u), f);
             sts128(to + (c >> 3) * Ly::KBLOCK + piece_at(y, c & 7), v.x, v.y, v.z, v.w);
           }
         } else {
           const uint32_t to = sm + Ly::OFF_V + b * Ly::VBYTES;
           const uint32_t* words = reinterpret_cast<const uint32_t*>(rows);
           if (lane < 16) {
-            sts128(to + piece_at(lane < 8 ? rz : rs, lane & 7), 0u, 0u, 0u, 0u);
-            sts128(to + Ly::VBLOCK + piece_at(lane < 8 ? rz : rs, lane & 7), 0u, 0u, 0u, 0u);
+            sts128(to + piece_at(lane < 8 ? rz : Ly::REST + vg, lane & 7), 0u, 0u, 0u, 0u);
+            sts128(to + Ly::VBLOCK + piece_at(lane < 8 ? rz : Ly::REST + vg, lane & 7), 0u, 0u, 0u, 0u);
           }
           // eight tokens of two channels: lanes take neighbouring channels of a token
 #pragma unroll 1
@@ -581,8 +613,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             for (int k = 0; k < 8; ++k) y[k] = 8 * piece + k < n_w ? words[(size_t)(8 * piece + k) * (D / 2) + c] : 0u;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint4 v = reorder8(make_uint4(__byte_perm(y[0], y[1], h ? 0x7632 : 0x5410), __byte_perm(y[2], y[3], h ? 0x7632 : 0x5410),
-                                                  __byte_perm(y[4], y[5], h ? 0x7632 : 0x5410), __byte_perm(y[6], y[7], h ? 0x7632 : 0x5410)), f, p.f16);
+              const uint4 v = reorder8<F16>(make_uint4(__byte_perm(y[0], y[1], h ? 0x7632 : 0x5410), __byte_perm(y[2], y[3], h ? 0x7632 : 0x5410),
+                                                  __byte_perm(y[4], y[5], h ? 0x7632 : 0x5410), __byte_perm(y[6], y[7], h ? 0x7632 : 0x5410)), f);
               sts128(to + (piece >> 3) * Ly::VBLOCK + piece_at(2 * c + h, piece & 7), v.x, v.y, v.z, v.w);
             }
           }
@@ -606,7 +638,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) x[i] = lds128(q_sm + k_row * QROW + group * (D / 2) + 16 * i);
       float f = 1.f;
-      if (!p.f16) {
+      if (!F16) {
         uint32_t m = 0u;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) m = top_of(m, x[i]);
@@ -620,7 +652,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       uint32_t y[D / 8];
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        const uint4 v = reorder8(x[i], f, p.f16);
+        const uint4 v = reorder8<F16>(x[i], f);
         y[4 * i] = v.x; y[4 * i + 1] = v.y; y[4 * i + 2] = v.z; y[4 * i + 3] = v.w;
       }
       tmem_st<D / 8>(row_t + Ly::COL_Q + group * (D / 8), y);
@@ -706,7 +738,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           tmem_ld<16>(row_t + Ly::COL_O + k, y);
           tc_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * (k == D && j == 8 ? f : fv));
+          for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * (k == D && j == Ly::ONES - D ? f : fv));
           tmem_st<16>(row_t + Ly::COL_O + k, y);
         }
       }
@@ -720,14 +752,31 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           const float off = m == -CUDART_INF_F ? 0.f : bias[x] + ((float)R_PEXP - m);
           const uint64_t oo = pair_of(off, off);
           uint32_t y[16];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
+          auto numerators = [&](int k, float (&v)[4]) {
             const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[4 * k]), __uint_as_float(s[4 * k + 1])), cc, oo));
             const float2 d = halves_of(fma2(pair_of(__uint_as_float(s[4 * k + 2]), __uint_as_float(s[4 * k + 3])), cc, oo));
-            y[2 * k] = pack_io2<true>(ex2(a.x), ex2(d.x));
-            y[2 * k + 1] = pack_io2<true>(ex2(a.y), ex2(d.y));
+            v[0] = ex2(a.x); v[1] = ex2(a.y); v[2] = ex2(d.x); v[3] = ex2(d.y);
+            y[2 * k] = pack_io2<true>(v[0], v[2]);
+            y[2 * k + 1] = pack_io2<true>(v[1], v[3]);
+          };
+          if constexpr (F16) {
+            uint32_t z[16];  // what the rounding left off
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float v[4];
+              numerators(k, v);
+              z[2 * k] = pack_io2<true>(v[0] - io2_lo<true>(y[2 * k]), v[2] - io2_hi<true>(y[2 * k]));
+              z[2 * k + 1] = pack_io2<true>(v[1] - io2_lo<true>(y[2 * k + 1]), v[3] - io2_hi<true>(y[2 * k + 1]));
+            }
+            tmem_st<16>(s_t + 32 * x + 16, z);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float v[4];
+              numerators(k, v);
+            }
           }
-          tmem_st<16>(s_t + 16 * x, y);
+          tmem_st<16>(s_t + 32 * x, y);
         }
         tc_wait_st();
       }
@@ -748,9 +797,9 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       uint32_t y[16];
       tmem_ld<16>(row_t + Ly::COL_O + D, y);
       tc_wait_ld();
-      l = N > 0 ? __uint_as_float(y[8]) * unit : 0.f;
+      l = N > 0 ? __uint_as_float(y[Ly::ONES - D]) * unit : 0.f;
 #pragma unroll
-      for (int x = 0; x < NG; ++x) extra[x] = __uint_as_float(y[x]) + (BV == 2 ? __uint_as_float(y[NG + x]) : 0.f);
+      for (int x = 0; x < NG; ++x) extra[x] = __uint_as_float(y[x]) + __uint_as_float(y[Ly::REST - D + x]);
     }
     const bool empty = N == 0;  // no token: the sums are not defined
     if (!empty && m == -CUDART_INF_F) m = CUDART_NAN_F;  // (no logit is a number, nor is the result)
@@ -777,7 +826,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       } else {
         uint32_t w[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = p.f16 ? pack_io2<true>(v[2 * j], v[2 * j + 1]) : pack_io2<false>(v[2 * j], v[2 * j + 1]);
+        for (int j = 0; j < 8; ++j) w[j] = F16 ? pack_io2<true>(v[2 * j], v[2 * j + 1]) : pack_io2<false>(v[2 * j], v[2 * j + 1]);
         sts128(mine + 2 * c0, w[0], w[1], w[2], w[3]);
         sts128(mine + 2 * c0 + 16, w[4], w[5], w[6], w[7]);
       }
@@ -801,10 +850,10 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   if (dead_sm != 0 && tid == 0) atomicExch(p.status, 1);
 }
 
-template <int D, int BK, int BV, int GS>
+template <int D, int BK, int BV, int GS, bool F16>
 cudaError_t rows_launch_one(const RowsParams& p, cudaStream_t st) {
   using Ly = RowsLayout<D, BK, BV, GS>;
-  auto kernel = rows_kernel<D, BK, BV, GS>;
+  auto kernel = rows_kernel<D, BK, BV, GS, F16>;
   constexpr size_t SMEM = Ly::TOTAL + 1024;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
   if (e != cudaSuccess) return e;
@@ -813,17 +862,17 @@ cudaError_t rows_launch_one(const RowsParams& p, cudaStream_t st) {
 
 }  // namespace
 
-template <int D>
+template <int D, bool F16>
 cudaError_t launch_rows_t(const RowsParams& p, cudaStream_t st) {
   switch (p.L.bk * 100 + p.L.bv * 10 + (p.dm.g == 64)) {
-    case 220: return rows_launch_one<D, 2, 2, 32>(p, st);
-    case 221: return rows_launch_one<D, 2, 2, 64>(p, st);
-    case 210: return rows_launch_one<D, 2, 1, 32>(p, st);
-    case 211: return rows_launch_one<D, 2, 1, 64>(p, st);
-    case 120: return rows_launch_one<D, 1, 2, 32>(p, st);
-    case 121: return rows_launch_one<D, 1, 2, 64>(p, st);
-    case 110: return rows_launch_one<D, 1, 1, 32>(p, st);
-    case 111: return rows_launch_one<D, 1, 1, 64>(p, st);
+    case 220: return rows_launch_one<D, 2, 2, 32, F16>(p, st);
+    case 221: return rows_launch_one<D, 2, 2, 64, F16>(p, st);
+    case 210: return rows_launch_one<D, 2, 1, 32, F16>(p, st);
+    case 211: return rows_launch_one<D, 2, 1, 64, F16>(p, st);
+    case 120: return rows_launch_one<D, 1, 2, 32, F16>(p, st);
+    case 121: return rows_launch_one<D, 1, 2, 64, F16>(p, st);
+    case 110: return rows_launch_one<D, 1, 1, 32, F16>(p, st);
+    case 111: return rows_launch_one<D, 1, 1, 64, F16>(p, st);
   }
   return cudaErrorInvalidValue;
 }

@@ -141,12 +141,12 @@ def _restored(cfg, K, V, layer, b, h):
     return k, v, ka, va
 
 
-def _reference(q, part, own, scale, seen_own):
+def _reference(q, part, own, scale, seen_own, pairs):
     """Softmax attention of one query vector over `part` (all tokens) and the first seen_own of `own`; and how far the kernels may
     be off, channel by channel.
 
     Over `part`: numerators rounded to half precision, off by at most 2^-11 each, under their own sum: |sum w e (v - out)| <=
-    2^-11 sum w |v - out|.  A logit: q as half precision relative to the row's largest element, below 2^-24 of it nothing is
+    2^-11 sum w |v - out|; pairs: to two halves, off by 2^-21 at most as far as the second one's subnormals reach, taken as 2^-18.  A logit: q as half precision relative to the row's largest element, below 2^-24 of it nothing is
     kept (sum 2^-25 max|q| |k|), and sums of fp32 that drop what lies below their last digit, one for each 16 products and
     the two of the bias: (D / 16 + 4) 2^-23 of the terms' sizes; an error d of the logits moves the result by at most
     2 d sum w |v - out|.  The value sums: one for each 16 tokens, twice at the join, 2^-23 of the terms' sizes each.
@@ -165,7 +165,7 @@ def _reference(q, part, own, scale, seen_own):
     if n:
         d = scale * ((D // 16 + 4) * 2.0 ** -23 * (ka[:n] @ np.abs(q)).max() + 2.0 ** -25 * np.abs(q).max() * ka[:n].sum(1).max())
         steps = n / 16 + 8
-        off += (2.0 ** -11 + 2 * d) * spread + steps * 2.0 ** -23 * (w[:n] @ va[:n])
+        off += (2.0 ** (-18 if pairs else -11) + 2 * d) * spread + steps * 2.0 ** -23 * (w[:n] @ va[:n])
     if seen_own:
         share = w[n:].sum()
         off += 2e-3 * share
@@ -174,8 +174,10 @@ def _reference(q, part, own, scale, seen_own):
     return out, off + 1e-6 * np.abs(out)
 
 
-def _check(cfg, out32, out16, q, restore_part, restore_own, T, own_len, heads=None, batch=None):
-    """Every row of the sequences and heads (all, or those named) against the reference.  restore_*(b, h): the stream's tokens."""
+def _check(cfg, out32, out16, q, restore_part, restore_own, T, own_len, heads=None, batch=None, rows=0):
+    """Every row of the sequences and heads (all, or those named) against the reference.  restore_*(b, h): the stream's tokens.
+    rows: of a kv head, more than the decode kernels take: half precision then goes with pairs."""
+    pairs = cfg.io_dtype == xq.XQ_F16 and rows > 16 * 8
     B, G = q.shape[1], cfg.n_q_heads // cfg.n_kv_heads
     scale = cfg.sm_scale if cfg.sm_scale > 0 else 1 / math.sqrt(cfg.head_dim)
     o32, o16, qd = out32.double().cpu().numpy(), out16.double().cpu().numpy(), q.double().cpu().numpy()
@@ -186,7 +188,7 @@ def _check(cfg, out32, out16, q, restore_part, restore_own, T, own_len, heads=No
             part, own = restore_part(b, h), restore_own(b, h)
             for j in range(T):
                 for a in range(h * G, (h + 1) * G):
-                    ref, off = _reference(qd[j, b, a], part, own, scale, max(0, own_len - T + j + 1))
+                    ref, off = _reference(qd[j, b, a], part, own, scale, max(0, own_len - T + j + 1), pairs)
                     err = np.abs(o32[j, b, a] - ref)
                     assert (err <= off).all(), (b, h, j, a, err.max(), off[err.argmax()])
                     assert (np.abs(o16[j, b, a] - ref) <= off + half * (np.abs(ref) + off) + 2.0 ** -25).all(), (b, h, j, a)
@@ -226,7 +228,7 @@ def _prefix_case(shape, kernel, P, each, Sp, S, T, seed=0, **more):
         o32 = cache.prefix_attention(prefix, layer, q.to(DEV), f32=True)
         o16 = cache.prefix_attention(prefix, layer, q.to(DEV))
         worst = _check(cc, o32, o16, q, lambda b, h: _restored(cp, kp, vp, layer, b // each, h),
-                       lambda b, h: _restored(cc, ko, vo, layer, b, h), T, S)
+                       lambda b, h: _restored(cc, ko, vo, layer, b, h), T, S, rows=T * each * cc.n_q_heads // cc.n_kv_heads)
         print(f"worst error / bound: {worst:.2f}")
     cache.check_device()
 
@@ -293,6 +295,14 @@ def test_prefix_more_rows_than_a_tile():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[4], SHAPES[6]])
+def test_half_precision_in_pairs(shape):
+    # more than 128 rows of a kv head, which no decode kernel takes; the prompt alone: its own tokens have a wider bound
+    _prefix_case(shape, xq.XQ_KERNEL_AUTO, 1, 3, 700, 0, 60)
+    _cross_case(shape, xq.XQ_KERNEL_AUTO, 2, 333, 70, lengths=[333, 140])
+
+
+@pytest.mark.gpu
 def test_prefix_empty_is_chunk_attention():
     cfg = _config(batch=2)
     K, V = _tokens(cfg, 1, 100)
@@ -317,7 +327,7 @@ def _cross_case(shape, kernel, B, S, T, lengths=None, seed=0, fill=None):
         o16 = cache.cross_attention(layer, q.to(DEV), lengths=ln)
         part = lambda b, h: [x[:n[b]] for x in _restored(cfg, K, V, layer, b, h)]  # noqa: E731
         none = [np.zeros((0, cfg.head_dim))] * 4
-        worst = _check(cfg, o32, o16, q, part, lambda b, h: none, T, 0)
+        worst = _check(cfg, o32, o16, q, part, lambda b, h: none, T, 0, rows=T * cfg.n_q_heads // cfg.n_kv_heads)
         print(f"worst error / bound: {worst:.2f}")
     cache.check_device()
 
@@ -392,7 +402,7 @@ def test_cross_more_tiles_than_half_the_device(B, T, f16, ragged):
     assert (o32 - want).abs().max() <= 2.0 ** -11 * 2 * V[1].abs().max().item() * 1.1
     none = [np.zeros((0, 128))] * 4
     for b, h in ((1, 0), (B - 1, 7), (B // 2, 3)):
-        _check(cfg, o32, o16, q, lambda b, h: [x[:n[b]] for x in _restored(cfg, K, V, 1, b, h)], lambda b, h: none, T, 0, heads=[h], batch=[b])
+        _check(cfg, o32, o16, q, lambda b, h: [x[:n[b]] for x in _restored(cfg, K, V, 1, b, h)], lambda b, h: none, T, 0, heads=[h], batch=[b], rows=4 * T)
     cache.check_device()
 
 
