@@ -104,7 +104,8 @@ typedef struct xq_config {
   int32_t n_splits;     /* sequence splits per (sequence, KV head) of a decode launch; 0 =
                            library chooses; at most XQ_MAX_SPLITS, and as many as there are
                            128-token batches.  The launch that xq_attention_chunk makes for
-                           many query tokens chooses its own                              */
+                           many query tokens, xq_prefix_attention (over the prefix) and
+                           xq_cross_attention choose their own                            */
   int32_t io_dtype;     /* type of K, V, q, out and of the residual window: XQ_BF16 or
                            XQ_F16                                                         */
   int32_t kernel;       /* XQ_KERNEL_*                                                    */
@@ -220,9 +221,10 @@ int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, in
  * one handle c are ordered by the caller, as all calls of a handle are.  A call captured into a graph keeps the
  * lengths it was captured with.
  * Precision: codes, scales and zero-points enter the matrix products exactly, q as half precision relative to
- * the row's largest element (exactly, if it is half precision), the softmax numerators rounded to half precision
- * where io_dtype is bfloat16 (at most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits
- * where it is half precision; sums are fp32.  Up to eight rows of a kv head: as xq_decode_attention.
+ * the row's largest element (exactly, if it is half precision), window tokens as half precision relative to the
+ * largest element of their 128, the softmax numerators rounded to half precision where io_dtype is bfloat16 (at
+ * most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits where it is half precision; sums
+ * are fp32.  Up to eight rows of a kv head: as xq_decode_attention.
  * XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.
  * The _f32 variant writes float results (tests).  Errors as xq_attention_chunk; XQ_ERR_ARG also: both layers
  * empty, 0 < S < n_q_tokens, current device not the handles'; XQ_ERR_CAPACITY: workspace too small. */
@@ -372,8 +374,8 @@ long long xq_pair_count(const xq_cache* c);
  * around each kernel.  xq_timing_enable(c, 1) allocates an event pool (host
  * call, not on the hot path) and clears the records; (c, 0) stops recording.
  * xq_timing_read synchronizes on the recorded events and returns, per kind
- * (0 decode split kernel, 1 merge kernel, 2 quantize-and-pack kernel, 3 window
- * append kernel), the launch count and total milliseconds. */
+ * (0 decode, chunk and rows kernels, 1 merge and join kernels, 2 quantize-and-pack
+ * kernel, 3 window append and gather kernels), the launch count and total milliseconds. */
 int xq_timing_enable(xq_cache* c, int on);
 int xq_timing_read(xq_cache* c, int kind, int* launches, double* total_ms);
 

@@ -50,6 +50,7 @@
 #pragma once
 #include "xq_internal.h"
 #include "xq_mma.cuh"
+#include "xq_shared.cuh"
 
 namespace xq {
 namespace {
@@ -269,8 +270,8 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, const DecodeLay
 // out = sum_s acc_s 2^(m_s-M) / sum_s l_s 2^(m_s-M).  No CTA ever waits for another.
 // What it takes is two trips to L2, one for all (m, l) and one for the partials: a warp that went through its share of
 // the heads one after the other, both trips for each, made it 2.3 us with four heads and 5.1 us with eight.
-// L, part_acc, part_ml: of the first of the CTA's NL layers; weights: NL * G * (ns + 1) floats of shared memory.  SHARED: a
-// stream may have no token at all, its result is zero.
+// L, part_acc, part_ml: of the first of the CTA's NL layers; weights: NL * G * (ns + 1) floats of shared memory, SHARED: G
+// more (what a row's own result is worth).
 template <int NL, bool SHARED>
 __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const DecodeLayer* L, int ns, int hk, int b,
                                              const float* part_acc, const float* part_ml, unsigned* ticket, int* s_flag,
@@ -318,8 +319,14 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
     if (lane == 0) {
-      w[ns] = SHARED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
-      if (NL == 1 && p.lse != nullptr) p.lse[SHARED ? shared_row(dm, p.each, b, hk, v) : row_of(v)] = M + log2f(Ls);
+      if constexpr (SHARED) {
+        const float2 f = with_own(p, shared_row(dm, p.each, b, hk, v), no_tokens(p, b), M, Ls);
+        w[ns] = f.x;
+        weights[dm.G * (ns + 1) + v] = f.y;
+      } else {
+        w[ns] = 1.0f / Ls;
+        if (NL == 1 && p.lse != nullptr) p.lse[row_of(v)] = M + log2f(Ls);
+      }
     }
   }
   __syncthreads();
@@ -343,7 +350,13 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
     }
     const float inv = w[ns];
     const int l = NL == 1 || v < dm.G ? 0 : 1;
-    store_out(p, L[l], SHARED ? shared_row(dm, p.each, b, hk, v) : hq0 + (v - l * dm.G), c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+    const float4 y = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    if constexpr (SHARED) {
+      const size_t to = shared_row(dm, p.each, b, hk, v);
+      store_out(p, L[l], to, c, add_own(p, to * D + c, y, weights[dm.G * (ns + 1) + v]));
+    } else {
+      store_out(p, L[l], hq0 + (v - l * dm.G), c, y);
+    }
   }
   if (threadIdx.x == 0) *ticket = 0u;  // ready for the next launch on this stream
 }
@@ -1325,10 +1338,14 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NL, MANY>::WARPS * 32, Pl
     for (int t = wrow0; t < wrow1; ++t) add(row((t + halves) % W, true));
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
-      if (SHARED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
-      const size_t to = SHARED ? shared_row(dm, p.each, b, hk, h) : hq;
-      store_out(p, LL[layer], to, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
-      if (NL == 1 && d == 0 && p.lse != nullptr) p.lse[to] = M + log2f(Ls);
+      if constexpr (SHARED) {
+        const size_t to = shared_row(dm, p.each, b, hk, h);
+        const float2 f = with_own(p, to, no_tokens(p, b), M, Ls);
+        store_out(p, LL[layer], to, d, add_own(p, to * D + d, make_float4(A.x * f.x, A.y * f.x, A.z * f.x, A.w * f.x), f.y));
+      } else {
+        store_out(p, LL[layer], hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
+        if (NL == 1 && d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
+      }
     } else {
       const size_t at = ((size_t)layer * dm.B * dm.Hq + hq) * p.ns_q + split;
       *reinterpret_cast<float4*>(part_acc + at * D + d) = A;

@@ -13,6 +13,7 @@
 #pragma once
 #include "xq_internal.h"
 #include "xq_mma.cuh"
+#include "xq_shared.cuh"
 
 namespace xq {
 namespace {
@@ -223,7 +224,7 @@ __device__ __forceinline__ void store_out(const DecodeParams& p, const DecodeLay
 // out = sum_s acc_s 2^(m_s-M) / sum_s l_s 2^(m_s-M).  No CTA ever waits for another.
 // What it takes is two trips to L2, one for all (m, l) and one for the partials: a warp that went through its share of
 // the heads one after the other, both trips for each, made it 2.3 us with four heads and 5.1 us with eight.
-// weights: G * (ns + 1) floats of shared memory.  SHARED: a stream may have no token at all, its result is zero.
+// weights: G * (ns + 1) floats of shared memory, SHARED: G more (what a row's own result is worth).
 template <bool SHARED>
 __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const DecodeLayer& L, int ns, int hk, int b,
                                              const float* part_acc, const float* part_ml, unsigned* ticket, int* s_flag,
@@ -270,8 +271,14 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
     if (lane == 0) {
-      w[ns] = SHARED && M == -CUDART_INF_F ? 0.f : 1.0f / Ls;
-      if (p.lse != nullptr) p.lse[SHARED ? shared_row(dm, p.each, b, hk, h) : hq0 + h] = M + log2f(Ls);
+      if constexpr (SHARED) {
+        const float2 f = with_own(p, shared_row(dm, p.each, b, hk, h), no_tokens(p, b), M, Ls);
+        w[ns] = f.x;
+        weights[dm.G * (ns + 1) + h] = f.y;
+      } else {
+        w[ns] = 1.0f / Ls;
+        if (p.lse != nullptr) p.lse[hq0 + h] = M + log2f(Ls);
+      }
     }
   }
   __syncthreads();
@@ -294,7 +301,13 @@ __device__ __forceinline__ void ticket_merge(const DecodeParams& p, const Decode
       }
     }
     const float inv = w[ns];
-    store_out(p, L, SHARED ? shared_row(dm, p.each, b, hk, h) : hq0 + h, c, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+    const float4 y = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+    if constexpr (SHARED) {
+      const size_t to = shared_row(dm, p.each, b, hk, h);
+      store_out(p, L, to, c, add_own(p, to * D + c, y, weights[dm.G * (ns + 1) + h]));
+    } else {
+      store_out(p, L, hq0 + h, c, y);
+    }
   }
   if (threadIdx.x == 0) *ticket = 0u;  // ready for the next launch on this stream
 }
@@ -1000,10 +1013,14 @@ __global__ void __launch_bounds__(Plan<BK, BV, GS, HP, NT>::WARPS * 32, Plan<BK,
     }
     const size_t hq = (size_t)b * dm.Hq + hk * G + h;
     if (ns == 1) {
-      if (SHARED && M == -CUDART_INF_F) Ls = 1.f;  // no token: zeros
-      const size_t to = SHARED ? shared_row(dm, p.each, b, hk, h) : hq;
-      store_out(p, L, to, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
-      if (d == 0 && p.lse != nullptr) p.lse[to] = M + log2f(Ls);
+      if constexpr (SHARED) {
+        const size_t to = shared_row(dm, p.each, b, hk, h);
+        const float2 f = with_own(p, to, no_tokens(p, b), M, Ls);
+        store_out(p, L, to, d, add_own(p, to * D + d, make_float4(A.x * f.x, A.y * f.x, A.z * f.x, A.w * f.x), f.y));
+      } else {
+        store_out(p, L, hq, d, make_float4(A.x / Ls, A.y / Ls, A.z / Ls, A.w / Ls));
+        if (d == 0 && p.lse != nullptr) p.lse[hq] = M + log2f(Ls);
+      }
     } else {
       *reinterpret_cast<float4*>(part_acc + (hq * p.ns_q + split) * D + d) = A;
       if (d == 0) *reinterpret_cast<float2*>(part_ml + (hq * p.ns_q + split) * 2) = make_float2(M, Ls);

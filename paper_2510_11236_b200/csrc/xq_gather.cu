@@ -156,7 +156,7 @@ static int place_lanes(int B) {
 }
 int gather_place_limit() { return PLACE_SMEM / (8 * 16 + 8); }
 
-cudaError_t launch_gather(const GatherParams& g, cudaStream_t st) {
+cudaError_t launch_gather(const GatherParams& g, cudaStream_t st, long long* launches) {
   const bool place = g.src == g.dst;
   Launch p;
   p.g = g;
@@ -171,6 +171,7 @@ cudaError_t launch_gather(const GatherParams& g, cudaStream_t st) {
   size_t total = 0;
   for (int i = 0; i < n; ++i) total += pieces(i);
   if (total == 0) return cudaSuccess;
+  ++*launches;
   // enough items for several CTAs on every SM
   constexpr size_t ENOUGH = 148 * 8 * 2;
   p.it.parts = place ? 1 : (int)std::min<size_t>(g.B_dst, std::max<size_t>(1, (ENOUGH + total - 1) / total));

@@ -502,6 +502,7 @@ int prepare_decode(const xq_cache* c, int layer, const void* q, void* out, int o
   p.shared = 0;
   p.each = 1;
   p.lengths = nullptr;
+  p.own = p.own_lse = nullptr;
   return XQ_OK;
 }
 
@@ -981,7 +982,9 @@ int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int ou
 
 // Query token j of n sees the cache up to its own position.  One launch of the chunk kernel, or (few tokens, the scalar
 // kernel) one decode launch per token, all on the same stream.
-int chunk_impl(xq_cache* c, int layer, const void* q, void* out, int n, int out_f32, void* stream, float* lse = nullptr) {
+// lse: as in ChunkParams.  chained: whether the last launch is a decode kernel's that one with late_wait may follow.
+int chunk_impl(xq_cache* c, int layer, const void* q, void* out, int n, int out_f32, void* stream, float* lse = nullptr,
+               bool* chained = nullptr) {
   if (!c || !q || !out) return XQ_ERR_ARG;
   if (layer < 0 || layer >= c->cfg.n_layers) return XQ_ERR_ARG;
   const int S = c->seq[layer];
@@ -1006,6 +1009,7 @@ int chunk_impl(xq_cache* c, int layer, const void* q, void* out, int n, int out_
                                lse ? lse + (size_t)j * dm.B * dm.Hq : nullptr);
     if (rc != XQ_OK) return rc;
   }
+  if (chained) *chained = chain;
   return XQ_OK;
 }
 }  // namespace
@@ -1115,15 +1119,14 @@ int launch_rows(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, i
   return e == cudaSuccess ? XQ_OK : fail_cuda(c, e);
 }
 
-int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_acc, const float* part_ml, const float* part_lse, const float* own,
-                     const float* own_lse, void* out, int out_f32, cudaStream_t st) {
+int launch_rows_join(xq_cache* c, const RowsPlan& r, int ns, const float* part_acc, const float* part_ml, const float* own, const float* own_lse,
+                     void* out, int out_f32, cudaStream_t st) {
   JoinParams p;
   p.rows = r.rows;
   p.D = c->cfg.head_dim;
   p.ns = ns;
   p.part_acc = part_acc;
   p.part_ml = part_ml;
-  p.part_lse = part_lse;
   p.own = own;
   p.own_lse = own_lse;
   p.out = out;
@@ -1167,9 +1170,11 @@ bool shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r
   return true;
 }
 
-// kv: the cache that is read; c: the handle whose scratch and status word the call uses.  lse: [T,Bq,Hq] or null.
+// kv: the cache that is read; c: the handle whose scratch and status word the call uses.  own, own_lse: the rows' results over
+// their own tokens, or null (joined here, a call of two tiny layers takes 6 us less than with a join kernel behind it).  chained: the
+// launch before made them and is a decode launch.
 int launch_shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, const SharedDecode& d, int T, const int* lengths,
-                         const void* q, void* out, int out_f32, float* lse, cudaStream_t st) {
+                         const void* q, void* out, int out_f32, const float* own, const float* own_lse, bool chained, cudaStream_t st) {
   const size_t rows = (size_t)(r.rows / T);
   const int S = kv->seq[layer];
   DecodeParams p;
@@ -1187,10 +1192,14 @@ int launch_shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsP
   p.shared = 1;
   p.each = r.each;
   p.lengths = lengths;
+  p.lse = nullptr;
+  // (a chained launch asks for tensor memory before its predecessor is done: only behind a kernel that has none)
+  const bool first_chained = chained && (d.dm.D == 64 || d.dm.G <= 4);
   for (int j = 0; j < T; ++j) {
     p.layer[0] = {layer_ptrs(kv, layer), (const uint16_t*)q + j * rows * d.dm.D, (uint8_t*)out + j * rows * d.dm.D * (out_f32 ? 4 : 2), nullptr, nullptr};
-    p.lse = lse ? lse + j * rows : nullptr;
-    p.early_fetch = p.late_wait = j > 0;  // what this launch reads was complete when the first one had waited
+    p.own = own ? own + j * rows * d.dm.D : nullptr;
+    p.own_lse = own ? own_lse + j * rows : nullptr;
+    p.early_fetch = p.late_wait = j > 0 || first_chained;  // what this launch reads was complete when the first one had waited
     const int rc = launch_decode(c, p, true, workspace_scratch(c), st);
     if (rc != XQ_OK) {
       c->tickets_clean = false;
@@ -1246,24 +1255,21 @@ int prefix_impl(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* o
   if (rc != XQ_OK) return rc;
   uint8_t* w = (uint8_t*)workspace;
   float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml), *own = nullptr, *lse = nullptr;
+  bool chained = false;
   if (S > 0) {
     own = (float*)(w + s.own);
     lse = (float*)(w + s.own_lse);
-    rc = chunk_impl(c, layer, q, own, T, 1, stream, lse);
+    rc = chunk_impl(c, layer, q, own, T, 1, stream, lse, &chained);
     if (rc != XQ_OK) return rc;
   }
   SharedDecode d;
-  if (shared_decode(c, prefix, layer, plan, d) && rows_one_by_one(prefix, layer, plan, d, T, ns)) {
-    if (S == 0) return launch_shared_decode(c, prefix, layer, plan, d, T, nullptr, q, out, out_f32, nullptr, st);
-    rc = launch_shared_decode(c, prefix, layer, plan, d, T, nullptr, q, acc, 1, ml, st);
-    if (rc != XQ_OK) return rc;
-    return launch_rows_join(c, plan, 1, acc, nullptr, ml, own, lse, out, out_f32, st);
-  }
+  if (shared_decode(c, prefix, layer, plan, d) && rows_one_by_one(prefix, layer, plan, d, T, ns))
+    return launch_shared_decode(c, prefix, layer, plan, d, T, nullptr, q, out, out_f32, own, lse, chained, st);
   // (one split of the prefix alone: the kernel writes the result)
   const bool direct = ns == 1 && S == 0 && c->cfg.kernel != XQ_KERNEL_GENERIC;
   rc = launch_rows(c, prefix, layer, plan, T, ns, nullptr, q, out, out_f32, direct ? nullptr : acc, ml, st);
   if (rc != XQ_OK || direct) return rc;
-  return launch_rows_join(c, plan, ns, acc, ml, nullptr, own, lse, out, out_f32, st);
+  return launch_rows_join(c, plan, ns, acc, ml, own, lse, out, out_f32, st);
 }
 
 int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const int32_t* lengths, int out_f32, void* workspace,
@@ -1289,11 +1295,11 @@ int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const in
   float *acc = (float*)(w + s.part_acc), *ml = (float*)(w + s.part_ml);
   SharedDecode d;
   if (shared_decode(c, c, layer, plan, d) && rows_one_by_one(c, layer, plan, d, T, ns))
-    return launch_shared_decode(c, c, layer, plan, d, T, lengths, q, out, out_f32, nullptr, st);
+    return launch_shared_decode(c, c, layer, plan, d, T, lengths, q, out, out_f32, nullptr, nullptr, false, st);
   const bool direct = ns == 1 && c->cfg.kernel != XQ_KERNEL_GENERIC;
   rc = launch_rows(c, c, layer, plan, T, ns, lengths, q, out, out_f32, direct ? nullptr : acc, ml, st);
   if (rc != XQ_OK || direct) return rc;
-  return launch_rows_join(c, plan, ns, acc, ml, nullptr, nullptr, nullptr, out, out_f32, st);
+  return launch_rows_join(c, plan, ns, acc, ml, nullptr, nullptr, out, out_f32, st);
 }
 
 // Whether a cache of `src`'s data can be held by `dst`: everything that decides what the bytes of a sequence mean.
@@ -1384,9 +1390,8 @@ int xq_gather_sequences(xq_cache* dst, const xq_cache* src, const int32_t* index
     cudaError_t e;
     {
       Timer t(dst, st, 3);
-      e = launch_gather(p, st);
+      e = launch_gather(p, st, &dst->launches);
     }
-    dst->launches++;
     if (e != cudaSuccess) return fail_cuda(dst, e);
   }
   for (int l = 0; l < L; ++l) dst->seq[l] = src->seq[l];

@@ -120,6 +120,9 @@ struct DecodeParams {
                        // times the heads of a kv head: "head" v of a kv head is head v % (G / each) of the sequence v / (G / each)
   int each;
   const int* lengths;  // [B] or null: the tokens of each sequence that exist
+  // [rows,D] and [rows], or null: the rows' results over other tokens (fp32, and their denominators as in lse), with which
+  // theirs are joined
+  const float *own, *own_lse;
   DecodeLayer layer[DECODE_MAX_LAYERS];
 };
 
@@ -184,14 +187,13 @@ struct RowsParams {
 };
 constexpr int ROWS_TILE = 128;
 
-// The splits' partials of each row (one whose reference is -infinity has no sums), and the row's result over other tokens where there is one (own: that result in fp32,
-// own_lse: its denominator as in DecodeParams), joined into out.  A row without tokens becomes zero.
+// The splits' partials of each row (one whose reference is -infinity has no sums), and the row's result over other tokens where
+// there is one (own: that result in fp32, own_lse: its denominator as in DecodeParams), joined into out.  A row without tokens becomes zero.
 struct JoinParams {
   long long rows;
   int D, ns;
   const float* part_acc;
   const float* part_ml;
-  const float* part_lse; // [rows] or null: there is one partial, a result with this denominator (as in DecodeParams)
   const float* own;      // [rows,D] or null
   const float* own_lse;  // [rows]
   void* out;
@@ -282,7 +284,7 @@ template <int D, bool F16>
 cudaError_t launch_rows_t(const RowsParams& p, cudaStream_t st);
 cudaError_t launch_rows_generic(const RowsParams& p, cudaStream_t st);
 cudaError_t launch_join(const JoinParams& p, cudaStream_t st);
-cudaError_t launch_gather(const GatherParams& p, cudaStream_t st);
+cudaError_t launch_gather(const GatherParams& p, cudaStream_t st, long long* launches);  // (none for empty caches)
 int gather_place_limit();  // sequences of a cache that can be reordered in place
 
 }  // namespace xq

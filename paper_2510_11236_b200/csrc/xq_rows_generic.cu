@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(ROW_WARPS * 32) rows_generic_kernel(const __gr
 #pragma unroll
   for (int j = 0; j < DPL; ++j) p.part_acc[(row * p.ns + split) * D + lane + 32 * j] = acc[j];
   if (lane == 0) {
-    p.part_ml[(row * p.ns + split) * 2] = m;
+    p.part_ml[(row * p.ns + split) * 2] = t1 > t0 && m == -CUDART_INF_F ? CUDART_NAN_F : m;  // (no logit is a number, nor is the result)
     p.part_ml[(row * p.ns + split) * 2 + 1] = l;
   }
 }
@@ -96,14 +96,13 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinP
   grid_dependency_wait();
   if (row >= p.rows) return;
   const float lse = p.own != nullptr ? p.own_lse[row] : -CUDART_INF_F;
-  auto state = [&](int s) { return p.part_lse != nullptr ? make_float2(p.part_lse[row], 1.f) : ml[s]; };
   float2 x[JOIN_SPLITS];
   float v[JOIN_SPLITS][DPL];
   auto fetch = [&](int s0) {
 #pragma unroll
     for (int k = 0; k < JOIN_SPLITS; ++k) {
       const bool there = s0 + k < p.ns;
-      x[k] = there ? state(s0 + k) : make_float2(-CUDART_INF_F, 0.f);
+      x[k] = there ? ml[s0 + k] : make_float2(-CUDART_INF_F, 0.f);
 #pragma unroll
       for (int j = 0; j < DPL; j += 2)
         *reinterpret_cast<float2*>(&v[k][j]) = there ? *reinterpret_cast<const float2*>(acc + (size_t)(s0 + k) * D + j) : make_float2(0.f, 0.f);

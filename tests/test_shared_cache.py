@@ -303,6 +303,61 @@ def test_half_precision_in_pairs(shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("each", [1, 2, 40])  # decode kernels, rows kernel
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[6]])
+def test_query_that_is_not_a_number(shape, each, kernel):
+    # its rows are not numbers, the others are as if it were one
+    cp, cc = _shape(shape, batch=1, max_seq=300, kernel=kernel), _shape(shape, batch=each, max_seq=40, kernel=kernel)
+    prefix, cache = _filled(cp, *_tokens(cp, 1, 300)), _filled(cc, *_tokens(cc, 2, 40))
+    alone = xq.Cache(cc, DEV)
+    q = _queries(cc, 3, 1).to(DEV)
+    bad = q.clone()
+    bad[0, each - 1, 5] = float("nan")
+    mine = torch.zeros(q.shape[:3], dtype=torch.bool, device=DEV)
+    mine[0, each - 1, 5] = True
+    for call in (lambda q: cache.prefix_attention(prefix, 0, q, f32=True), lambda q: alone.prefix_attention(prefix, 0, q, f32=True)):
+        want, got = call(q), call(bad)
+        assert got[mine].isnan().all()
+        assert torch.equal(got[~mine], want[~mine])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,each", [(SHAPES[0], 2), (SHAPES[3], 2), (SHAPES[7], 1), (SHAPES[4], 1)])
+@pytest.mark.parametrize("T", [1, 2])
+def test_prefix_few_rows_one_after_the_other(shape, each, T):
+    # launches of a call and of the next one overlap: each call's result is that of the call by itself, eager and from a graph
+    cp, cc = _shape(shape, batch=3, max_seq=900), _shape(shape, batch=3 * each, max_seq=300)
+    prefix, cache = _filled(cp, *_tokens(cp, 1, 900)), _filled(cc, *_tokens(cc, 2, 270))
+    qs = [_queries(cc, 10 + i, T).to(DEV) for i in range(12)]
+    work = torch.empty(xq.xq_prefix_workspace_bytes(cache.handle, prefix.handle, T), dtype=torch.uint8, device=DEV)
+    want = []
+    for i, q in enumerate(qs):
+        want.append(cache.prefix_attention(prefix, i % 2, q, f32=True, workspace=work))
+        torch.cuda.synchronize()
+    outs = [torch.empty_like(w) for w in want]
+
+    def run():
+        for i, q in enumerate(qs):
+            cache.prefix_attention(prefix, i % 2, q, out=outs[i], f32=True, workspace=work)
+    for _ in range(20):
+        for o in outs:
+            o.zero_()
+        run()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(20):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    cache.check_device()
+
+
+@pytest.mark.gpu
 def test_prefix_empty_is_chunk_attention():
     cfg = _config(batch=2)
     K, V = _tokens(cfg, 1, 100)
