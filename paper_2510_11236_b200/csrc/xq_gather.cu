@@ -1,5 +1,7 @@
 // Copies of sequences between two caches, or within one: sequence b of the destination becomes sequence index[b] of the
-// source, in all layers and regions (codes, scales and zero-points, windows).  Nothing is computed; bound: HBM.
+// source, in all layers and regions (codes, scales and zero-points, windows).  Nothing is computed; bound: HBM.  A prompt of 8192
+// tokens to 32 sequences, 8 layers (1.06 GB written): 175 us, 6.2 TB/s; 17 of 24 sequences of 4100 tokens to another cache (1.15 GB
+// moved): 179 us, 6.4 TB/s.  In place, 16 beams of 1000 tokens, 32 layers: 45 to 58 us, by the share of them that changes.
 //
 // A region of a stream is one contiguous run of bytes, and the layouts of two caches differ in the streams' spacing alone,
 // so a work item is a piece of (layer, region, kv head) with the sequences it goes to.

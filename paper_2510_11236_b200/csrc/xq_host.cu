@@ -121,9 +121,9 @@ void make_plan(const xq_config* c, Plan& pl) {
 }
 
 // Rows calls (prefix and cross attention): CTAs that splits make, at most, in waves of the device; and times, us: of a CTA's
-// batch, of its start and end, of a join, of a row's partial.
+// batch (half precision: pairs of numerators), of its start and end, of a join, of a row's partial.
 constexpr int ROWS_WAVES = 4;
-constexpr double ROWS_BATCH = 1.28, ROWS_FIXED = 9.9, ROWS_JOIN = 2.5, ROWS_PART = 1.8e-4;
+constexpr double ROWS_BATCH = 1.28, ROWS_BATCH_F16 = 1.5, ROWS_FIXED = 9.9, ROWS_JOIN = 2.5, ROWS_PART = 1.8e-4;
 
 constexpr int N_KINDS = 4;
 constexpr int TIMING_POOL = 1 << 15;
@@ -1052,8 +1052,8 @@ RowsPlan rows_plan(const xq_cache* kv, int Bq, int T) {
 // partials are written and read again.
 double rows_time(const xq_cache* kv, const RowsPlan& r, int S, int ns) {
   const int batches = (S + 127) / 128;
-  const double waves = ceil((double)(r.ctas * ns) / kv->sm_count);
-  return waves * (ROWS_BATCH * ((batches + ns - 1) / ns) + ROWS_FIXED) + (ns > 1 ? ROWS_JOIN + ROWS_PART * (double)r.rows * ns : 0.0);
+  const double waves = ceil((double)(r.ctas * ns) / kv->sm_count), batch = kv->cfg.io_dtype == XQ_F16 ? ROWS_BATCH_F16 : ROWS_BATCH;
+  return waves * (batch * ((batches + ns - 1) / ns) + ROWS_FIXED) + (ns > 1 ? ROWS_JOIN + ROWS_PART * (double)r.rows * ns : 0.0);
 }
 int rows_splits(const xq_cache* kv, const RowsPlan& r, int S) {
   const int most = std::min(rows_most_splits(kv, r.ctas), std::max(1, (S + 127) / 128));
@@ -1210,7 +1210,8 @@ int launch_shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsP
 }
 
 // Whether T decode launches take less time than one rows call: modelled times in us, decode as plan_batches has them, rows as
-// rows_splits does.
+// rows_splits does.  (One token against 16 inputs of 1500, 32 kv heads of one head: 25 us a layer, the rows kernel 67; 16 tokens
+// against one of 40000, four heads: the rows kernel 39 us.)
 bool rows_one_by_one(const xq_cache* kv, int layer, const RowsPlan& r, const SharedDecode& d, int T, int ns) {
   return T <= 16 && d.plan.alone + (T - 1) * d.plan.next < rows_time(kv, r, kv->seq[layer], ns);
 }

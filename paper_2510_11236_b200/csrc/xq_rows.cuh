@@ -28,6 +28,17 @@
 // (four keys, four values), one issues products, one copies packed data.  Window tokens go into the same operands as they are,
 // bfloat16 ones scaled by a power of two for each batch.
 //
+// Bound: not one pipe, but two chains of latencies that compete for issue slots (60 to 70 % of them, tensor pipe 41 %).  A batch of
+// 128 tokens takes 1.24 to 1.30 us a CTA, 2400 cycles (head_dim 128, bfloat16; half precision 1.50), whether 9 or 128 rows exist,
+// and a launch 10 us more.  Cycles of a batch: the products 1152 (half precision 1728).  S from its issue to the softmax warps 870,
+// the search 900, the turn 500, the numerators 1700, to the issuing warp 250, and two batches are in flight.  The expansion of a
+// batch's keys 2000 and 600 until the next one, values the same.  In copies: half of the expansion left out 0.57 us a tile for
+// 0.63.  Measured and not kept, us a tile against 0.62: three expanding groups of four warps that take keys and values in turn 0.64;
+// products and barriers of S a tile at a time, so that the next S waits for one tile's numerators 0.66, with three groups 0.76;
+// 32 columns of S kept in registers through the turn 0.64; numerators by single multiply-adds 0.65; runs of tiles over several
+// streams for 148 resident CTAs 0.69 (prompts of 100 tokens behind 16k 2 % faster, 200 tokens behind 6404 11 % slower).
+// Before: two softmax groups 0.69, one for all 128 tokens 0.83, an O and a reference for each of two groups 0.89.
+//
 // Every wait on an mbarrier is bounded, as in the chunk kernel: a thread that gives up sets a flag that ends the others' waits,
 // and the CTA reports through the status word.
 #pragma once
