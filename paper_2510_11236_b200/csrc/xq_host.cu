@@ -1097,6 +1097,8 @@ int launch_rows(xq_cache* c, const xq_cache* kv, int layer, const RowsPlan& r, i
   p.r = residual_count(S, dm.R);
   p.n_q = S - p.r;
   p.lengths = lengths;
+  // (200 tokens against four sequences of ragged lengths up to 6404, two layers, mean of eight draws: 224 -> 199 us)
+  p.longest_first = lengths != nullptr && dm.B <= 32 && r.ctas * ns > kv->sm_count;
   p.T = T;
   p.each = r.each;
   p.row_tiles = r.row_tiles;

@@ -173,6 +173,8 @@ struct RowsParams {
   const uint16_t* q;   // [T,Bq,Hq,D], Bq = B * each
   int n_q, r;          // tokens of the cache: packed, window
   const int* lengths;  // [B] or null: the tokens of each sequence that exist
+  int longest_first;   // CTAs take the sequences by their lengths, the longest one first: where they go in waves, the last ones
+                       // then end together (at most 32 sequences; the scalar kernel does not look at it)
   int T, each;
   int row_tiles;       // per (sequence, kv head): T * each * G rows over ROWS_TILE
   int ns;              // splits of the tokens

@@ -225,6 +225,17 @@ __device__ __forceinline__ int window_exponent(float mx) {
   return (mx >= 0.0625f && mx < 32768.f) || !(mx > 0.f) ? 0 : 14 - exponent_of(mx);
 }
 
+// The sequence with the k-th longest length (of n <= 32; among equals the first).  All lanes of a warp.
+__device__ __forceinline__ int by_length(const int* lengths, int n, int S, int k, int lane) {
+  const int mine = lane < n ? max(0, min(S, lengths[lane])) : -1;
+  int rank = 0;
+  for (int j = 0; j < n; ++j) {
+    const int other = __shfl_sync(0xffffffffu, mine, j);
+    rank += other > mine || (other == mine && j < lane);
+  }
+  return __ffs(__ballot_sync(0xffffffffu, lane < n && rank == k)) - 1;
+}
+
 template <int D, int BK, int BV, int GS, bool F16>
 __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constant__ RowsParams p) {
   using Ly = RowsLayout<D, BK, BV, GS>;
@@ -289,21 +300,27 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   }
   // ---- the CTA's rows and batches ----
   const int G = dm.G;
-  const int split = blockIdx.x % p.ns, rest = blockIdx.x / p.ns, rt = rest % p.row_tiles, bh = rest / p.row_tiles;
-  const int u = bh / dm.Hkv, hk = bh - u * dm.Hkv;
+  const int split = blockIdx.x % p.ns, rest = blockIdx.x / p.ns, rt = rest % p.row_tiles;
+  int bh = rest / p.row_tiles, u = bh / dm.Hkv;
+  const int hk = bh - u * dm.Hkv;
   const int row0 = rt * ROWS_TILE, n_rows = min(ROWS_TILE, p.T * p.each * G - row0);
   auto call_row = [&](int k) {  // of the stream's row row0 + k
     const int x = row0 + k, h = x % G, ji = x / G, i = ji % p.each, j = ji / p.each;
     return ((size_t)j * (dm.B * p.each) + (size_t)u * p.each + i) * dm.Hq + hk * G + h;
   };
   const int my_row = 8 * warp + (lane & 7);  // of q, for the warps that fetch it
-  const uint32_t my_call_row = warp < 4 * R_GROUPS && my_row < n_rows ? (uint32_t)call_row(my_row) : 0u;
+  uint32_t my_call_row = warp < 4 * R_GROUPS && my_row < n_rows ? (uint32_t)call_row(my_row) : 0u;
 
   // (tensor memory is asked for after the wait: a CTA of the preceding kernel that shares the SM may still have to get its own)
   grid_dependency_wait();
   grid_dependents_go();
   if (warp == R_MMA) tmem_alloc((uint32_t)__cvta_generic_to_shared(&tmem_base_sm), 512u);
   int n_q = p.n_q, r = p.r;
+  if (p.longest_first) {
+    u = by_length(p.lengths, dm.B, n_q + r, u, lane);
+    bh = u * dm.Hkv + hk;
+    if (warp < 4 * R_GROUPS && my_row < n_rows) my_call_row = (uint32_t)call_row(my_row);
+  }
   if (p.lengths != nullptr) {
     const int S = max(0, min(n_q + r, p.lengths[u]));
     n_q = min(n_q, S);

@@ -462,6 +462,28 @@ def test_cross_more_tiles_than_half_the_device(B, T, f16, ragged):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B", [1, 3, 31, 32, 33])
+@pytest.mark.parametrize("kind", ["equal", "none", "two", "rising", "out of range"])
+def test_cross_order_of_lengths(B, kind):
+    # more CTAs than the device takes at once: they go by length, up to 32 sequences.  Against the scalar kernel, as above.
+    T, S = 8000 // B, 300
+    kw = dict(batch=B, n_q_heads=4, n_kv_heads=2, max_seq=S)
+    cfg, other = _config(**kw), _config(kernel=xq.XQ_KERNEL_GENERIC, **kw)
+    K, V = _tokens(cfg, B, S)
+    cache, slow = _filled(cfg, K, V), _filled(other, K, V)
+    n = {"equal": [S] * B, "none": [0] * B, "two": [S if b % 3 else 65 for b in range(B)], "rising": [1 + b * 9 for b in range(B)],
+         "out of range": [[-7, 2 ** 31 - 1, -2 ** 31, 128][b % 4] for b in range(B)]}[kind]
+    lengths = torch.tensor(n, dtype=torch.int32, device=DEV)
+    q = _queries(cfg, 3, T).to(DEV)
+    got, want = (c.cross_attention(0, q, lengths=lengths, f32=True) for c in (cache, slow))
+    assert (got - want).abs().max() <= 2.0 ** -11 * 2 * V[0].abs().max().item() * 1.1
+    for b in range(B):
+        if n[b] <= 0:
+            assert not got[:, b].any()
+    cache.check_device()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("shape,P", [(SHAPES[0], 1), (SHAPES[3], 5)])
 def test_prefix_more_tiles_than_half_the_device(shape, P):
     # 8 sequences of 40 tokens behind each prompt, eight kv heads
