@@ -173,6 +173,8 @@ struct RowsParams {
   const uint16_t* q;   // [T,Bq,Hq,D], Bq = B * each
   int n_q, r;          // tokens of the cache: packed, window
   const int* lengths;  // [B] or null: the tokens of each sequence that exist
+  int late_wait;       // 1: the preceding launch is a decode launch of the same call, over other tokens, which has waited for all
+                       // that this one reads and writes: it need not be over before this one begins, only before it ends
   int longest_first;   // CTAs take the sequences by their lengths, the longest one first: where they go in waves, the last ones
                        // then end together (at most 32 sequences; the scalar kernel does not look at it)
   int T, each;

@@ -311,8 +311,9 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   const int my_row = 8 * warp + (lane & 7);  // of q, for the warps that fetch it
   uint32_t my_call_row = warp < 4 * R_GROUPS && my_row < n_rows ? (uint32_t)call_row(my_row) : 0u;
 
-  // (tensor memory is asked for after the wait: a CTA of the preceding kernel that shares the SM may still have to get its own)
-  grid_dependency_wait();
+  // (tensor memory is asked for after the wait: a CTA of the preceding kernel that shares the SM may still have to get its own;
+  // late_wait: a decode kernel, whose CTAs have theirs when this one starts)
+  if (!p.late_wait) grid_dependency_wait();
   grid_dependents_go();
   if (warp == R_MMA) tmem_alloc((uint32_t)__cvta_generic_to_shared(&tmem_base_sm), 512u);
   int n_q = p.n_q, r = p.r;
@@ -880,6 +881,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
     }
   }
+  if (p.late_wait) grid_dependency_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();

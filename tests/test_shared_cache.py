@@ -323,9 +323,10 @@ def test_query_that_is_not_a_number(shape, each, kernel):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("shape,each", [(SHAPES[0], 2), (SHAPES[3], 2), (SHAPES[7], 1), (SHAPES[4], 1)])
+@pytest.mark.parametrize("shape,each", [(SHAPES[0], 2), (SHAPES[3], 2), (SHAPES[7], 1), (SHAPES[4], 1),
+                                        (SHAPES[0], 12), (SHAPES[7], 8), (SHAPES[4], 9), (SHAPES[5], 2)])  # (rows kernel)
 @pytest.mark.parametrize("T", [1, 2])
-def test_prefix_few_rows_one_after_the_other(shape, each, T):
+def test_prefix_calls_one_after_the_other(shape, each, T):
     # launches of a call and of the next one overlap: each call's result is that of the call by itself, eager and from a graph
     cp, cc = _shape(shape, batch=3, max_seq=900), _shape(shape, batch=3 * each, max_seq=300)
     prefix, cache = _filled(cp, *_tokens(cp, 1, 900)), _filled(cc, *_tokens(cc, 2, 270))
