@@ -102,8 +102,11 @@ __device__ __forceinline__ float2 halves_of(uint64_t a) {
 __device__ __forceinline__ void arrive_if(bool p, uint32_t bar) {
   asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(bar), "r"((uint32_t)p) : "memory");
 }
-// barrier of the softmax warps
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 512;\n" ::: "memory"); }
+// barriers of the softmax warps; of the loading warp, which has initialised the mbarriers, with the expanding warps; and with
+// the others
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, %0;\n" ::"n"(R_GROUPS * 128) : "memory"); }
+__device__ __forceinline__ void expand_sync() { asm volatile("bar.sync 2, %0;\n" ::"n"((2 * R_EXPAND + 1) * 32) : "memory"); }
+__device__ __forceinline__ void start_sync() { asm volatile("bar.sync 3, %0;\n" ::"n"(R_GROUPS * 128 + 64) : "memory"); }
 // A warp's bounded wait.  What follows when the first look fails is out of line: most looks do not, and the kernel's roles
 // share an instruction cache.
 __device__ __noinline__ bool warp_wait_longer(uint32_t bar, uint32_t parity, volatile int* dead) {
@@ -225,6 +228,20 @@ __device__ __forceinline__ int window_exponent(float mx) {
   return (mx >= 0.0625f && mx < 32768.f) || !(mx > 0.f) ? 0 : 14 - exponent_of(mx);
 }
 
+// Eight rows of 16 LANES bytes from shared memory, 16 bytes apart more than that: a warp's, the first one `first`.  to_row: of
+// lane k, where row `first` + k goes, in strides.
+template <int LANES>
+__device__ __forceinline__ void store_rows(uint32_t from, uint8_t* to, size_t stride, uint32_t to_row, int first, int n_rows, int lane) {
+  constexpr int AT_ONCE = 32 / LANES;
+#pragma unroll
+  for (int k = 0; k < 8 / AT_ONCE; ++k) {
+    const int y = k * AT_ONCE + lane / LANES;
+    const uint32_t row = __shfl_sync(0xffffffffu, to_row, y);
+    const uint4 v = lds128(from + (first + y) * (16 * LANES + 16) + lane % LANES * 16);
+    if (first + y < n_rows) *reinterpret_cast<uint4*>(to + row * stride + lane % LANES * 16) = v;
+  }
+}
+
 // The sequence with the k-th longest length (of n <= 32; among equals the first).  All lanes of a warp.
 __device__ __forceinline__ int by_length(const int* lengths, int n, int S, int k, int lane) {
   const int mine = lane < n ? max(0, min(S, lengths[lane])) : -1;
@@ -298,6 +315,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     dead_sm = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
+  const bool expands = warp >= 4 * R_GROUPS && warp < R_MMA;
+  if (expands || warp == R_LOAD) expand_sync();
   // ---- the CTA's rows and batches ----
   const int G = dm.G;
   const int split = blockIdx.x % p.ns, rest = blockIdx.x / p.ns, rt = rest % p.row_tiles;
@@ -351,7 +370,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     bulk_load(dst + Ly::RAW_VC, reinterpret_cast<const uint8_t*>(p.L.v_codes) + (size_t)bh * ((size_t)dm.nq_cap * (D * BV / 8)) + t * (16 * D * BV), 16 * D * BV, bar);
     bulk_load(dst + Ly::RAW_VM, reinterpret_cast<const uint8_t*>(p.L.v_meta) + (size_t)bh * ((size_t)dm.nq_cap * 4 * NG) + t * (RB * 4 * NG), RB * 4 * NG, bar);
   };
-  // Before the CTA's first barrier: the first packed batches, and q's rows into the second key operand's place, eight rows a
+  // Before the barrier: the first packed batches, and q's rows into the second key operand's place, eight rows a
   // warp, lanes along a row.
   constexpr int QROW = 2 * D + 16;
   static_assert(ROWS_TILE * QROW <= Ly::KBYTES, "q fits");
@@ -375,10 +394,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       sts128(q_sm + (first + k * AT_ONCE + lane / PIECES) * QROW + lane % PIECES * 16, x[k].x, x[k].y, x[k].z, x[k].w);
   }
 
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tbase = tmem_base_sm;
+  // (the expanding warps need nothing of this, the first batch is expanded meanwhile: with the stores below 70.7 -> 68.0 us for
+  // eight samples of each of four prompts of 5000, two layers)
+  uint32_t tbase = 0u;
+  if (!expands) {
+    tc_fence_before();
+    start_sync();
+    tc_fence_after();
+    tbase = tmem_base_sm;
+  }
 
   if (warp == R_MMA) {
     // ================= products: the loop is warp-uniform, one elected lane issues =================
@@ -841,10 +865,9 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     }
     const bool empty = N == 0;  // no token: the sums are not defined
     if (!empty && m == -CUDART_INF_F) m = CUDART_NAN_F;  // (no logit is a number, nor is the result)
-    const bool store = k_row < n_rows && dead_sm == 0;
     const float inv = p.part_acc != nullptr ? uv : uv / l;
     const bool wide = p.part_acc != nullptr || p.out_f32;
-    // through shared memory (the operands' place), so that a row leaves in one piece
+    // through shared memory (the operands' place), so that a warp stores whole rows (a bulk copy a row was slower)
     const uint32_t row_bytes = wide ? 4 * D : 2 * D, mine = sm + k_row * (row_bytes + 16);
 #pragma unroll 1
     for (int k = 0; k < D / 4; k += 16) {
@@ -869,16 +892,14 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         sts128(mine + 2 * c0 + 16, w[4], w[5], w[6], w[7]);
       }
     }
-    proxy_fence();
     softmax_sync();
-    if (group == 0 && store) {
-      const size_t to_row = call_row(k_row);
-      uint8_t* const to = p.part_acc != nullptr ? reinterpret_cast<uint8_t*>(p.part_acc + (to_row * p.ns + split) * D)
-                                                : reinterpret_cast<uint8_t*>(p.out) + to_row * row_bytes;
-      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n" ::"l"(to), "r"(mine), "r"(row_bytes) : "memory");
-      asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
-      if (p.part_acc != nullptr) reinterpret_cast<float2*>(p.part_ml)[to_row * p.ns + split] = make_float2(m, empty ? 0.f : l);
-      asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
+    if (dead_sm == 0) {
+      const int ns = p.part_acc != nullptr ? p.ns : 1;
+      uint8_t* const to = (p.part_acc != nullptr ? reinterpret_cast<uint8_t*>(p.part_acc) : reinterpret_cast<uint8_t*>(p.out)) + (size_t)(ns > 1 ? split : 0) * row_bytes;
+      if (wide) store_rows<D / 4>(sm, to, (size_t)ns * row_bytes, my_call_row, 8 * warp, n_rows, lane);
+      else store_rows<D / 8>(sm, to, (size_t)ns * row_bytes, my_call_row, 8 * warp, n_rows, lane);
+      if (p.part_acc != nullptr && group == 0 && k_row < n_rows)
+        reinterpret_cast<float2*>(p.part_ml)[(size_t)call_row(k_row) * p.ns + split] = make_float2(m, empty ? 0.f : l);
     }
   }
   if (p.late_wait) grid_dependency_wait();
