@@ -124,7 +124,7 @@ struct Plan {
   static_assert(!PARK || (CTAS * TMEM <= 512 && (TMEM & (TMEM - 1)) == 0), "tensor memory");
   static constexpr int TOTAL = room(WARPS);
   static_assert(TOTAL <= 228 * 1024 / CTAS - 1024 - 512, "shared memory");
-  static_assert(WARPS * WARP >= VH * (256 + 1) * 4, "the merge's weights");
+  static_assert(WARPS * WARP >= VH * (256 + 2) * 4, "the merge's weights");
 };
 
 // The code operand pair: the code bits at BASE + BITS * i of both halves of w as they are, fp16 subnormals; their weight is

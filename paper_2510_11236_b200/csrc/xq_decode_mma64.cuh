@@ -66,7 +66,7 @@ struct Plan {
   static constexpr int WARPS = room(MOST) <= LIMIT ? MOST : (room(MOST - 1) <= LIMIT ? MOST - 1 : MOST - 2);
   static constexpr int TOTAL = room(WARPS);
   static_assert(TOTAL <= LIMIT, "shared memory");
-  static_assert(WARPS * WARP >= HP * NT * (256 + 1) * 4, "the merge's weights");
+  static_assert(WARPS * WARP >= HP * NT * (256 + 2) * 4, "the merge's weights");
 };
 
 // Code operands: (code - center) * weight * 2^-9, normal numbers, center = (2^BITS - 1) / 2.

@@ -158,15 +158,16 @@ struct MergeParams {
   float* lse;  // [B,Hq] or null: as in DecodeParams
 };
 
-// Attention of query rows over all tokens of a cache, none masked but for the sequences' lengths (xq_rows.cuh).  Sequence u
-// of the cache serves the sequences u * each .. u * each + each - 1 of the queries.  A row is (token j, one of these
-// sequences i, head h of a kv head): row (j * each + i) * G + h of its stream, and row (j * Bq + u * each + i) * Hq + hk * G
-// + h of the call.
 // Row of the call's q and result for "head" v of kv head hk and sequence u of the cache (DecodeParams::shared).
 __host__ __device__ inline size_t shared_row(const Dims& dm, int each, int u, int hk, int v) {
   const int heads = dm.G / each;
   return ((size_t)u * each + v / heads) * (dm.Hkv * heads) + hk * heads + v % heads;
 }
+
+// Attention of query rows over all tokens of a cache, none masked but for the sequences' lengths (xq_rows.cuh).  Sequence u
+// of the cache serves the sequences u * each .. u * each + each - 1 of the queries.  A row is (token j, one of these
+// sequences i, head h of a kv head): row (j * each + i) * G + h of its stream, and row (j * Bq + u * each + i) * Hq + hk * G
+// + h of the call.
 struct RowsParams {
   Dims dm;             // of the cache (B: its sequences)
   LayerPtrs L;
@@ -192,7 +193,8 @@ struct RowsParams {
 constexpr int ROWS_TILE = 128;
 
 // The splits' partials of each row (one whose reference is -infinity has no sums), and the row's result over other tokens where
-// there is one (own: that result in fp32, own_lse: its denominator as in DecodeParams), joined into out.  A row without tokens becomes zero.
+// there is one (own: that result in fp32, own_lse: its denominator as in DecodeParams), joined into out.  A row without tokens
+// becomes zero.
 struct JoinParams {
   long long rows;
   int D, ns;
