@@ -123,7 +123,7 @@ void make_plan(const xq_config* c, Plan& pl) {
 // Rows calls (prefix and cross attention): CTAs that splits make, at most, in waves of the device; and times, us: of a CTA's
 // batch (half precision: pairs of numerators), of its start and end, of a join, of a row's partial.
 constexpr int ROWS_WAVES = 4;
-constexpr double ROWS_BATCH = 1.28, ROWS_BATCH_F16 = 1.5, ROWS_FIXED = 9.9, ROWS_JOIN = 2.5, ROWS_PART = 1.8e-4;
+constexpr double ROWS_BATCH = 1.28, ROWS_BATCH_F16 = 1.5, ROWS_FIXED = 8.9, ROWS_JOIN = 2.5, ROWS_PART = 1.8e-4;
 
 constexpr int N_KINDS = 4;
 constexpr int TIMING_POOL = 1 << 15;
