@@ -222,7 +222,8 @@ int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, in
  * lengths it was captured with.
  * Precision: codes, scales and zero-points enter the matrix products exactly, q as half precision relative to
  * the row's largest element (exactly, if it is half precision), window tokens as half precision relative to the
- * largest element of their 128, the softmax numerators rounded to half precision where io_dtype is bfloat16 (at
+ * largest element of their 128 (values below 2^-46 of larger ones before them, packed ones counted as 1: to 2^-85 of
+ * those), the softmax numerators rounded to half precision where io_dtype is bfloat16 (at
  * most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits where it is half precision; sums
  * are fp32.  Up to eight rows of a kv head: as xq_decode_attention.
  * XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.

@@ -223,10 +223,17 @@ __device__ __forceinline__ uint32_t top_of(uint32_t m, const uint4& v) {
 }
 __device__ __forceinline__ float bf16_top(uint32_t m) { return __uint_as_float(max(m & 0xffffu, m >> 16) << 16); }
 
-// exponent that puts a window's largest magnitude into the range of half precision, 0 where it is there
-__device__ __forceinline__ int window_exponent(float mx) {
-  return (mx >= 0.0625f && mx < 32768.f) || !(mx > 0.f) ? 0 : 14 - exponent_of(mx);
+// exponent that puts a window batch's largest magnitude into the range of half precision, 0 where it is there; at most `most`
+// (126: its power of two and the inverse are normal numbers)
+__device__ __forceinline__ int window_exponent(float mx, int most) {
+  return min((mx >= 0.0625f && mx < 32768.f) || !(mx > 0.f) ? 0 : 14 - exponent_of(mx), most);
 }
+// 2^e for e from -256 to 127, 0 below the normal numbers
+__device__ __forceinline__ float pow2_or_zero(int e) { return e < -126 ? 0.f : pow2i(e); }
+// What the exponent of a window batch's values may exceed that of any batch before it by, packed ones (0) among them.  O is
+// brought to it: without a batch's own scale its sums are below 2^64 (numerators 2^15, values 2^18, 2^31 tokens), and so stay
+// below 2^124.  Smaller values have an error of up to 2^-85 of the largest ones before them.
+constexpr int R_RISE = 60;
 
 // Eight rows of 16 LANES bytes from shared memory, 16 bytes apart more than that: a warp's, the first one `first`.  to_row: of
 // lane k, where row `first` + k goes, in strides.
@@ -258,9 +265,10 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   using Ly = RowsLayout<D, BK, BV, GS>;
   constexpr int NG = Ly::NG;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 2 + 2 * 4 + 4 * R_GROUPS + 2 * R_UNITS + 2];
+  __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 2 + 2 * 4 + 4 * R_GROUPS + 3 * R_UNITS + 2];
   __shared__ float top_sm[R_GROUPS][ROWS_TILE], m_sm[ROWS_TILE];  // largest element of a quarter of a row of q; softmax reference
   __shared__ uint32_t unit_sm[R_UNITS][2][R_EXPAND];        // window batch, keys / values: largest magnitude of each expanding warp
+  __shared__ int value_e_sm[R_UNITS];                       // window batch: exponent of its values
   __shared__ uint32_t tmem_base_sm;
   __shared__ volatile int dead_sm;
 
@@ -280,7 +288,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   const uint32_t bar_turn = bar_o + 32;                  // [4 warps][R_GROUPS] the reference for a group's next tile is there
   const uint32_t bar_kunit = bar_turn + 32 * R_GROUPS;              // [R_UNITS] the magnitudes of a window batch's keys are known
   const uint32_t bar_vunit = bar_kunit + 8 * R_UNITS;    // [R_UNITS] the same of its values
-  const uint32_t bar_q = bar_vunit + 8 * R_UNITS;        // Q is written
+  const uint32_t bar_ve = bar_vunit + 8 * R_UNITS;       // [R_UNITS] the exponent of its values is there
+  const uint32_t bar_q = bar_ve + 8 * R_UNITS;           // Q is written
   const uint32_t bar_end = bar_q + 8;                    // every product is complete
 
   if (tid == 32 * R_LOAD) {
@@ -309,6 +318,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     for (int i = 0; i < R_UNITS; ++i) {
       mbar_init(bar_kunit + 8 * i, R_EXPAND);
       mbar_init(bar_vunit + 8 * i, R_EXPAND);
+      mbar_init(bar_ve + 8 * i, 1);
     }
     mbar_init(bar_q, 4 * R_GROUPS);
     mbar_init(bar_end, 1);
@@ -351,14 +361,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   share_of(all_batches, p.ns, split, t_lo, t_hi);
   const int N = t_hi - t_lo;
   const int n_pk = max(0, min(t_hi, pk_batches) - t_lo);  // packed batches of the range; batch i is window batch i - n_pk
-  // exponent of a window batch's keys (0) or values (1)
-  auto batch_exponent = [&](int i, int which) {
+  // exponent of a window batch's keys (which = 0), of its values (1)
+  auto batch_exponent = [&](int i, int which, int most) {
     const uint32_t* m = unit_sm[(i - n_pk) % R_UNITS][which];
     uint32_t x = 0u;
 #pragma unroll
     for (int k = 0; k < R_EXPAND; ++k) x = max(x, m[k]);
-    return F16 ? 0 : window_exponent(bf16_top(x));
+    return F16 ? 0 : window_exponent(bf16_top(x), most);
   };
+  auto value_exponent = [&](int i) { return F16 ? 0 : value_e_sm[(i - n_pk) % R_UNITS]; };
 
   // a batch's packed data into its raw stage
   auto load = [&](int i) {
@@ -521,6 +532,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       fields[j] = (bits == 2 ? 0x00030003u : 0x00010001u) << (bits * j);
       if (BK != BV) asm volatile("" : "+r"(fields[j]));
     }
+    int most = n_pk > 0 ? R_RISE : 126;  // for the next window batch's exponent of the values
 #pragma unroll 1
     for (int i = 0; i < N; ++i) {
       const int b = i & 1;
@@ -648,8 +660,12 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         if (lane == 0) mbar_arrive(bar_unit);
         if (!F16) {
           if (!warp_wait(bar_unit, ((i - n_pk) / R_UNITS) & 1, &dead_sm)) break;
-          f = pow2i(batch_exponent(i, keys ? 0 : 1));
+          const int e = batch_exponent(i, keys ? 0 : 1, keys ? 126 : most);
+          f = pow2i(e);
+          most = min(most, e + R_RISE);
+          if (!keys && ew == 0 && lane == 0) value_e_sm[slot_w] = e;
         }
+        arrive_if(!keys && ew == 0 && lane == 0, bar_ve + 8 * slot_w);
         if (keys) {
           // (the extra rows of a window batch's keys are not looked at)
           const uint32_t to = sm + b * Ly::KBYTES;
@@ -732,7 +748,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       if (!warp_wait(bar_s + 8 * b, turn, &dead_sm)) break;
       if (!packed) {
         const int slot = (i - n_pk) % R_UNITS, round = ((i - n_pk) / R_UNITS) & 1;
-        if (!warp_wait(bar_kunit + 8 * slot, round, &dead_sm) || !warp_wait(bar_vunit + 8 * slot, round, &dead_sm)) break;
+        if (!warp_wait(bar_kunit + 8 * slot, round, &dead_sm) || !warp_wait(bar_ve + 8 * slot, round, &dead_sm)) break;
       }
       tc_fence_after();
       const int n_valid = (packed ? n_q - (t_lo + i) * RB : r - (t_lo + i - pk_batches) * RB) - RT * g;  // of this tile
@@ -759,7 +775,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
             if (32 * x < n_valid) bias[x] = (__uint_as_float(z) + (BK == 2 ? __uint_as_float(y) : 0.f)) * cq;
           }
         } else {
-          c *= pow2i(-batch_exponent(i, 0));
+          c *= pow2i(-batch_exponent(i, 0, 126));
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -787,13 +803,13 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       __syncwarp();
       arrive_if(lane == 0, next_turn);
       // the exponent of the values in O changes with a batch's first tile
-      const int de = packed || g > 0 ? 0 : batch_exponent(i, 1) - (i > n_pk ? batch_exponent(i - 1, 1) : 0);
+      const int de = packed || g > 0 ? 0 : value_exponent(i) - (i > n_pk ? value_exponent(i - 1) : 0);
       if ((i > 0 || g > 0) && !idle && __any_sync(0xffffffffu, m != m_old || de != 0)) {
         // O has to follow a raised reference, and the scale of the window's values: after the products of the tile before
         const int j = g ? i : i - 1;
         if (!warp_wait(bar_o + 16 * (j & 1) + 8 * (1 - g), (j >> 1) & 1, &dead_sm)) break;
         tc_fence_after();
-        const float f = m_old == -CUDART_INF_F ? 0.f : ex2(m_old - m), fv = f * pow2i(de);
+        const float f = m_old == -CUDART_INF_F ? 0.f : ex2(m_old - m), fv = f * pow2_or_zero(de);
 #pragma unroll 1
         for (int k = 0; k < Ly::VN; k += 16) {
           uint32_t y[16];
@@ -852,8 +868,8 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     softmax_sync();  // (every warp comes here, whatever failed)
     tc_fence_after();
     float m = N > 0 ? m_sm[k_row] : -CUDART_INF_F;
-    const int ev = N > n_pk ? batch_exponent(N - 1, 1) : 0;
-    const float unit = pow2i(-R_PEXP), uv = unit * pow2i(-ev);
+    const int ev = N > n_pk ? value_exponent(N - 1) : 0;
+    const float unit = pow2i(-R_PEXP), back = pow2i(-ev);
     float l = 0.f, extra[NG];
     {
       uint32_t y[16];
@@ -865,7 +881,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     }
     const bool empty = N == 0;  // no token: the sums are not defined
     if (!empty && m == -CUDART_INF_F) m = CUDART_NAN_F;  // (no logit is a number, nor is the result)
-    const float inv = p.part_acc != nullptr ? uv : uv / l;
+    const float inv = p.part_acc != nullptr ? unit : unit / l;  // (times `back` it may be below the normal numbers)
     const bool wide = p.part_acc != nullptr || p.out_f32;
     // through shared memory (the operands' place), so that a warp stores whole rows (a bulk copy a row was slower)
     const uint32_t row_bytes = wide ? 4 * D : 2 * D, mine = sm + k_row * (row_bytes + 16);
@@ -879,7 +895,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
 #pragma unroll
       for (int x = 1; x < NG; ++x) z = c0 / GS == x ? extra[x] : z;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = empty ? 0.f : (__uint_as_float(y[j]) + z) * inv;
+      for (int j = 0; j < 16; ++j) v[j] = empty ? 0.f : (__uint_as_float(y[j]) + z) * inv * back;
       if (wide) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)

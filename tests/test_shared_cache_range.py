@@ -1,0 +1,148 @@
+"""Prefix and cross attention over caches of unusual magnitude, window, length and sharing pattern, against plain 64-bit attention
+over what the oracle's packing restores."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_11236_b200 as xq
+from tests import util
+from tests.test_shared_cache import DEV, KERNELS, SHAPES, _filled, _queries, _restored, _shape, _tokens
+
+BLOCK = 128  # tokens whose window rows share an exponent
+
+
+def _exponent(mx):
+    """Power of two that the kernels scale a block of bfloat16 window rows by: its largest magnitude into half precision's range."""
+    return 0 if 0.0625 <= mx < 32768.0 or mx == 0.0 else 14 - math.floor(math.log2(mx))
+
+
+def _window_steps(x, n, rise):
+    """What half precision leaves of window rows x[n:], taken relative to the largest of their 128: at most half a step of its
+    subnormal numbers, 2^-25, in the block's scale, token by token.  rise: a block is scaled by at most 2^60 more than any before
+    it, packed tokens counted with 2^0 (values)."""
+    off, most = np.zeros(len(x)), 60 if n else 126
+    for a in range(n, len(x), BLOCK):
+        e = min(_exponent(np.abs(x[a:a + BLOCK]).max()), most if rise else 126)
+        most = min(most, e + 60)
+        off[a:a + BLOCK] = 2.0 ** (-25 - e)
+    return off
+
+
+def _expect(q, k, v, ka, va, n, scale, pairs, f16, products=1):
+    """Attention of the rows q [rows, D] over k, v (n of them packed) and how far the kernels may be off.
+
+    Numerators: half precision, 2^-11 of each, under their own sum (pairs: 2^-18); below 2^-14 of the largest number that half
+    precision has for them a fixed 2^-25: they are scaled by 2^7 against a reference that the largest logit is at most one (log2)
+    below, so 2^-31 of the largest weight.  Logits: q as half precision relative to the row's largest (2^-25), window keys as above,
+    and (D / 16 + 4) sums of fp32 that drop their last digit, each of `products` times.  Value sums: one for each 16 tokens,
+    `products` times, twice at the join."""
+    S, D = k.shape
+    kw, vw = (np.zeros(S), np.zeros(S)) if f16 else (_window_steps(k, n, False), _window_steps(v, n, True))
+    out, off = np.zeros(q.shape), np.zeros(q.shape)
+    for r, row in enumerate(q):
+        x = scale * (k @ row)
+        w = np.exp(x - x.max())
+        w /= w.sum()
+        o = w @ v
+        away = np.abs(v - o)
+        top = np.abs(row).max()
+        d = scale * (products * (D // 16 + 4) * 2.0 ** -23 * (ka @ np.abs(row)).max() + 2.0 ** -25 * top * ka.sum(1).max()
+                     + kw.max() * np.abs(row).sum())
+        steps = products * S / 16 + 8
+        out[r] = o
+        off[r] = ((2.0 ** (-18 if pairs else -11) + 2 * d) * (w @ away) + 2.0 ** -31 * w.max() * away.sum(0)
+                  + steps * 2.0 ** -23 * (w @ va) + w @ vw + 1e-6 * np.abs(o) + 2.0 ** -60 * np.abs(v).max())
+    return out, off
+
+
+def _compare(cfg, o32, o16, q, restored, n, heads, batch, pairs, products=1, tokens=None):
+    """Rows of the named sequences, kv heads and query tokens against _expect; restored(b, h): a stream's (k, v, ka, va)."""
+    G, f16 = cfg.n_q_heads // cfg.n_kv_heads, cfg.io_dtype == xq.XQ_F16
+    scale = cfg.sm_scale if cfg.sm_scale > 0 else 1 / math.sqrt(cfg.head_dim)
+    o32, o16, qd = o32.double().cpu().numpy(), o16.double().cpu().numpy(), q.double().cpu().numpy()
+    half, worst = torch.finfo(q.dtype).eps / 2, 0.0
+    at = list(range(len(qd))) if tokens is None else tokens
+    for b in batch:
+        for h in heads:
+            k, v, ka, va = restored(b, h)
+            rows = [x[at, b, h * G:(h + 1) * G].reshape(-1, cfg.head_dim) for x in (qd, o32, o16)]
+            ref, off = _expect(rows[0], k, v, ka, va, n, scale, pairs, f16, products)
+            err = np.abs(rows[1] - ref)
+            assert (err <= off).all(), (b, h, err.max(), off.reshape(-1)[np.nan_to_num(err / off, nan=np.inf).argmax()])
+            assert (np.abs(rows[2] - ref) <= off + half * (np.abs(ref) + off) + 2.0 ** -25).all(), (b, h)
+            worst = max(worst, (err / off).max())
+    print(f"worst error / bound: {worst:.2f}")
+
+
+# ---- windows ----
+
+# window capacity, tokens, size of each block of 128 window rows
+WINDOWS = [
+    (128, 300, [1e-30]), (128, 300, [1e-35]), (128, 300, [1e-39]), (128, 300, [0.0]), (128, 300, [1e5]), (128, 300, [1e30]),
+    (512, 1000, [1.0, 1e-30, 1e4, 1e-4]), (512, 1000, [1e20, 1e-30, 1.0, 1e-38]), (512, 480, [1e-38, 1e-30, 1e-36, 1.0]),
+    (512, 400, [1e30, 1e-38, 1e-38, 1e-38]), (512, 500, [1e-36] * 4),
+    (1024, 2000, [1.0, 1e-3, 1e3, 1e-5, 1e5, 1.0, 1e-2, 1e2]),
+    (4096, 8100, [10.0 ** (3 * (i * 7 % 5) - 6) for i in range(32)]),
+]
+
+
+def _sized(x, r, sizes):
+    """The last r tokens of every [batch, heads, S, D] tensor in x, block by block times `sizes`."""
+    S = x[0].shape[2]
+    f = torch.ones(S)
+    for i, s in enumerate(sizes):
+        f[S - r + i * BLOCK:S - r + (i + 1) * BLOCK] = s
+    return [(t.float() * f[:, None]).to(t.dtype) for t in x]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("T", [1, 17, 1300])  # decode kernels, rows kernel, and so many rows that a CTA takes all the tokens
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[3]])
+@pytest.mark.parametrize("R,S,sizes", WINDOWS)
+def test_window_values_of_every_size(R, S, sizes, shape, T, kernel):
+    D, Hq, Hkv, g, _, kq, vq, f16 = shape
+    cfg = _shape((D, Hq, Hkv, g, R, kq, vq, f16), batch=2, max_seq=S, kernel=kernel)
+    K, V = _tokens(cfg, 1, S)
+    r = (S - 1) % R + 1
+    V = _sized(V, r, sizes)
+    cache = _filled(cfg, K, V)
+    q = _queries(cfg, 3, T)
+    o32, o16 = cache.cross_attention(1, q.to(DEV), f32=True), cache.cross_attention(1, q.to(DEV))
+    _compare(cfg, o32, o16, q, lambda b, h: _restored(cfg, K, V, 1, b, h), S - r, [0, 1], [0, 1], False, tokens=[0, T - 1])
+    cache.check_device()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("T", [1, 17, 1300])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[3]])
+@pytest.mark.parametrize("R,S,sizes", [w for w in WINDOWS if max(w[2]) <= 1e5] + [(128, 300, [3e8])])
+def test_window_keys_of_every_size(R, S, sizes, shape, T, kernel):
+    # queries so small that the largest keys' logits are of ordinary size
+    D, Hq, Hkv, g, _, kq, vq, f16 = shape
+    cfg = _shape((D, Hq, Hkv, g, R, kq, vq, f16), batch=2, max_seq=S, kernel=kernel)
+    K, V = _tokens(cfg, 1, S, outliers=False)
+    r = (S - 1) % R + 1
+    K = _sized(K, r, sizes)
+    cache = _filled(cfg, K, V)
+    q = (_queries(cfg, 3, T).float() / max(1.0, *sizes)).to(torch.bfloat16)
+    o32, o16 = cache.cross_attention(1, q.to(DEV), f32=True), cache.cross_attention(1, q.to(DEV))
+    _compare(cfg, o32, o16, q, lambda b, h: _restored(cfg, K, V, 1, b, h), S - r, [0, 1], [0, 1], False, tokens=[0, T - 1])
+    cache.check_device()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [SHAPES[1], SHAPES[6]])
+def test_long_windows_in_half_precision(shape):
+    D, Hq, Hkv, g, _, kq, vq, f16 = shape
+    cfg = _shape((D, Hq, Hkv, g, 1024, kq, vq, f16), batch=2, max_seq=2000)
+    K, V = _tokens(cfg, 1, 2000)
+    V = _sized(V, 976, [1.0, 1e-3, 1e3, 1e-4, 1e4, 1.0, 1e-2, 1e2])
+    cache = _filled(cfg, K, V)
+    q = _queries(cfg, 3, 60)
+    o32, o16 = cache.cross_attention(1, q.to(DEV), f32=True), cache.cross_attention(1, q.to(DEV))
+    _compare(cfg, o32, o16, q, lambda b, h: _restored(cfg, K, V, 1, b, h), 1024, [0, 1], [0, 1], True, tokens=[0, 31, 59])
+    cache.check_device()
