@@ -220,8 +220,9 @@ int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, in
  * no length changes), contents arbitrary; calls that may overlap on the GPU need one each, and calls through
  * one handle c are ordered by the caller, as all calls of a handle are.  A call captured into a graph keeps the
  * lengths it was captured with.
- * Precision: codes, scales and zero-points enter the matrix products exactly, q as half precision relative to
- * the row's largest element (exactly, if it is half precision), window tokens as half precision relative to the
+ * Precision: codes, scales and zero-points enter the matrix products exactly (2-bit ones beside a scale above 32752 in
+ * the same 128 tokens to 2^-23), q as half precision relative to the row's largest element (exactly, if it is half
+ * precision), window tokens as half precision relative to the
  * largest element of their 128 (values below 2^-46 of larger ones before them, packed ones counted as 1: to 2^-85 of
  * those), the softmax numerators rounded to half precision where io_dtype is bfloat16 (at
  * most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits where it is half precision; sums

@@ -15,6 +15,9 @@
 // which then has none, as two rows hi + lo.  16 tokens at 40000, half precision, error in the result's norm, whose own rounding is
 // 2.07e-4: 2.61e-4 with o = 1, z and s; 2.45e-4 with hi + lo alone; 2.07e-4 with both.
 //
+// Where 2 s would pass half precision's largest number (s above 32752), the operand holds a quarter of all that, and its product is
+// made four times (keys: of a batch, values: of a tile).  Exact but for s and z below 2^-12 beside such scales.
+//
 // Q: half precision, scaled by a power of two for each row (exact for bfloat16 down to 2^-16 of the row's largest element).
 // P: the softmax numerators times 2^R_PEXP, in half precision, rounded for bfloat16 results (2e-4 of the result's norm, an eighth
 // of the result's own rounding; divided by the sum of the rounded P), as pairs hi + lo, a product each, for half-precision ones.
@@ -60,6 +63,7 @@ constexpr int R_EXPAND = 4;      // expanding warps of a kind: keys 16 .. 19, va
 constexpr int R_MMA = 24, R_LOAD = 25, R_THREADS = 26 * 32;
 constexpr int R_UNITS = 4;       // window batches whose exponents are kept
 constexpr uint32_t MAX_DOUBLED = 0x77ff;  // the largest half-precision number whose double is finite
+constexpr uint32_t QUARTERS = 0x34003400;  // two of 1 / 4
 
 // shared-memory matrix descriptor, K-major, 128-byte swizzle: rows of 128 bytes, groups of eight 1024 bytes apart
 __device__ __forceinline__ uint64_t rows_desc(uint32_t addr) {
@@ -190,25 +194,6 @@ __device__ __forceinline__ void expand_rows(const uint32_t (&w)[N], int shift, c
     expand_rows<BITS, OFFSET, ODD, N, K + 1>(w, shift, s0, s1, dst0, dst1, f);
   }
 }
-// Eight of them where a scale is too large to be doubled: c s + z, rounded (the operand's extra rows are then zero).  w:
-// shifted so that the first field is at bit 0; s_at, z_at: where the parameters of element j are in shared memory.
-template <int BITS, typename S, typename Z>
-__device__ __forceinline__ void restore8(uint32_t w, S s_at, Z z_at, uint32_t dst) {
-  uint32_t o[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {  // word k: elements (0, 2), (1, 3), (4, 6), (5, 7)
-    const int e = (k >> 1) * 4 + (k & 1);
-    float v[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint32_t c = (w >> (8 * ((e & 3) + 2 * x) + BITS * (e >> 2))) & ((1u << BITS) - 1u);
-      v[x] = fmaf((float)c, f16_to_f(lds16(s_at(e + 2 * x))), f16_to_f(lds16(z_at(e + 2 * x))));
-    }
-    o[k] = pack_io2<true>(v[0], v[1]);
-  }
-  sts128(dst, o[0], o[1], o[2], o[3]);
-}
-
 // eight 16-bit numbers times f, as half precision in the operands' order: elements (0, 2), (1, 3), (4, 6), (5, 7)
 template <bool F16>
 __device__ __forceinline__ uint4 reorder8(const uint4& v, float f) {
@@ -222,6 +207,11 @@ __device__ __forceinline__ uint32_t top_of(uint32_t m, const uint4& v) {
   return __vmaxu2(__vmaxu2(__vmaxu2(m, v.x & 0x7fff7fffu), __vmaxu2(v.y & 0x7fff7fffu, v.z & 0x7fff7fffu)), v.w & 0x7fff7fffu);
 }
 __device__ __forceinline__ float bf16_top(uint32_t m) { return __uint_as_float(max(m & 0xffffu, m >> 16) << 16); }
+
+// whether one of the scales in two halves, in any lane's, is too large to be doubled
+__device__ __forceinline__ bool any_large(uint32_t scales) {
+  return __any_sync(0xffffffffu, max(scales & 0xffffu, scales >> 16) > MAX_DOUBLED);
+}
 
 // exponent that puts a window batch's largest magnitude into the range of half precision, 0 where it is there; at most `most`
 // (126: its power of two and the inverse are normal numbers)
@@ -268,6 +258,7 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
   __shared__ __align__(8) unsigned long long bar_mem[2 * R_RAW + 4 * R_BUFS + 2 + 2 * 4 + 4 * R_GROUPS + 3 * R_UNITS + 2];
   __shared__ float top_sm[R_GROUPS][ROWS_TILE], m_sm[ROWS_TILE];  // largest element of a quarter of a row of q; softmax reference
   __shared__ uint32_t unit_sm[R_UNITS][2][R_EXPAND];        // window batch, keys / values: largest magnitude of each expanding warp
+  __shared__ volatile uint32_t quarter_sm[2][R_BUFS];       // keys, values: an expanded batch's parts (values: bits of its tiles) that are quarters
   __shared__ int value_e_sm[R_UNITS];                       // window batch: exponent of its values
   __shared__ uint32_t tmem_base_sm;
   __shared__ volatile int dead_sm;
@@ -436,14 +427,20 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           if (elect_one()) {
             const uint64_t v = rows_desc(smu + Ly::OFF_V + b * Ly::VBYTES + g * Ly::VBLOCK);
             const uint32_t P = dS + g * RT;
-            bool sum = i > 2 || g > 0;
-            if constexpr (F16) {  // the rests first: a sum drops what lies below its own last digit
+            auto product = [&](bool sum) {
+              if constexpr (F16) {  // the rests first: a sum drops what lies below its own last digit
 #pragma unroll
-              for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, P + p_col(ks) + 16, v + 2 * ks, IDV, sum || ks > 0);
-              sum = true;
+                for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, P + p_col(ks) + 16, v + 2 * ks, IDV, sum || ks > 0);
+                sum = true;
+              }
+#pragma unroll
+              for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, P + p_col(ks), v + 2 * ks, IDV, sum || ks > 0);
+            };
+            product(i > 2 || g > 0);
+            if (BV == 2 && (quarter_sm[1][b] >> g & 1u)) {
+#pragma unroll 1
+              for (int k = 0; k < 3; ++k) product(true);
             }
-#pragma unroll
-            for (int ks = 0; ks < RT / 16; ++ks) rows_mma(tb + Ly::COL_O, P + p_col(ks), v + 2 * ks, IDV, sum || ks > 0);
             rows_commit(bar_o + 16 * b + 8 * g);
             if (g == 1) rows_commit(bar_vfree + 8 * b);
           }
@@ -457,8 +454,15 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         tc_fence_after();
         if (elect_one()) {
           const uint64_t k = rows_desc(smu + b * Ly::KBYTES);
+          auto product = [&](bool sum) {
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) rows_mma(dS, tb + Ly::COL_Q + 8 * ks, k + (ks / 4) * (Ly::KBLOCK / 16) + 2 * (ks % 4), IDK, ks > 0);
+            for (int ks = 0; ks < D / 16; ++ks) rows_mma(dS, tb + Ly::COL_Q + 8 * ks, k + (ks / 4) * (Ly::KBLOCK / 16) + 2 * (ks % 4), IDK, sum || ks > 0);
+          };
+          product(false);
+          if (BK == 2 && quarter_sm[0][b] != 0u) {
+#pragma unroll 1
+            for (int x = 0; x < 3; ++x) product(true);
+          }
           rows_commit(bar_s + 8 * b);
           rows_commit(bar_kfree + 8 * b);
         }
@@ -509,18 +513,22 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
     // what a lane reads, from the raw stage's start, and writes, from the operand's
     const uint32_t code_off = keys ? slot0 * (32 * Ly::KROW) + word * 4 / CB * (32 * CB) + word * 4 % CB + sub * CB
                                    : Ly::RAW_VC + (BV == 2 ? o * 4 : o / 2 * 4) + (v_c0 + sub) * 16;
-    const uint32_t meta_off = keys ? Ly::RAW_KM + 2 * (lane * (D / 32) + 2 * kb) : Ly::RAW_VM + lane * (4 * NG) + 2 * vg;
+    const uint32_t meta_off = keys ? Ly::RAW_KM + 2 * (lane * (D / 32) + 2 * kb) : Ly::RAW_VM + lane * (4 * NG);
     const uint32_t op_off = keys ? kb * Ly::KBLOCK : Ly::OFF_V;
     const int at = (lane & ~3) | ((lane & 1) << 1) | ((lane >> 1) & 1);  // place of channel `lane`: elements of four 0, 2, 1, 3
     const uint32_t params_off = keys ? piece_at(rz, at >> 3) + 2 * (at & 7) : piece_at(lane & 2 ? rz : rs, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;
     const uint32_t rest_off = piece_at(Ly::REST + vg, lane >> 3) + ((lane >> 2) & 1) * 8 + (lane & 1) * 4;  // values
     const uint32_t row_off = piece_at(row, 2 * o), scales_off = piece_at(rs, 2 * o);
     static_assert(PARTS <= 2 && RB % 8 == 0, "rows rz + 2 x: bit 1 of rz is clear where x can be 1");
-    if (!keys && ew < 2 && lane < 8) {  // the row that sums the numerators
-      for (int b = 0; b < R_BUFS; ++b)
-        sts128(sm + Ly::OFF_V + b * Ly::VBYTES + ew * Ly::VBLOCK + piece_at(Ly::ONES, lane), 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
+    // the row that sums the numerators: of tile ew of a batch, ones, or quarters where the rest of the operand is
+    auto write_ones = [&](int b, uint32_t ones) {
+      if (lane < 8) sts128(sm + Ly::OFF_V + b * Ly::VBYTES + ew * Ly::VBLOCK + piece_at(Ly::ONES, lane), ones, ones, ones, ones);
+    };
+    if (!keys && ew < 2) {
+      for (int b = 0; b < R_BUFS; ++b) write_ones(b, 0x3c003c00u);
       proxy_fence();
     }
+    uint32_t quarter_ones = 0u;  // bit b: of buffer b they are quarters
     __syncwarp();
     // The codes' fields: an instruction has room for one constant and the expansion needs two, so these are kept in registers.
     // Where keys and values have one width the compiler does that (2-bit keys, 1-bit values, 128 rows: 0.644 -> 0.623 us a tile;
@@ -552,21 +560,43 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
       }
       const uint32_t raw = sm + Ly::OFF_RAW + (i % R_RAW) * Ly::RAW;
       const uint32_t dst = sm + op_off + b * (keys ? Ly::KBYTES : Ly::VBYTES);
+      const int valid = n_q - (t_lo + i) * RB;  // tokens of a packed batch that exist
+      uint32_t quarter = 0u;                    // keys: the batch is in quarters; values: bit x, tile x is
       if (packed && keys) {
         // parameters of channels 64 kb + lane and 32 more, side by side in the group's order, to the operand's rows
-        uint32_t sw[PARTS], zw[PARTS], large = 0u;  // bit x: of slot x
+        uint32_t sw[PARTS], zw[PARTS];
 #pragma unroll
         for (int x = 0; x < PARTS; ++x) {
           const uint32_t meta = raw + meta_off + (slot0 + x) * 32 / GS * (4 * D);
           sw[x] = lds32(meta);
           zw[x] = lds32_at<2 * D>(meta);
         }
+        if constexpr (BK == 2) {
+          // the largest of all the batch's scales (each of the four warps looks at all of them: they have to agree)
+          uint32_t top = 0u;
+#pragma unroll
+          for (int x = 0; x < RB / GS; ++x) {
+            if (x * GS < valid) {
+              const uint32_t scales = raw + Ly::RAW_KM + x * (4 * D) + lane * (D / 16);
+              if constexpr (D == 128) {
+                const uint2 v = lds64(scales);
+                top = __vmaxu2(top, __vmaxu2(v.x, v.y));
+              } else {
+                top = __vmaxu2(top, lds32(scales));
+              }
+            }
+          }
+          if (any_large(top)) {
+            quarter = 1u;
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) {
+              sw[x] = hmul2(sw[x], QUARTERS);
+              zw[x] = hmul2(zw[x], QUARTERS);
+            }
+          }
+        }
 #pragma unroll
         for (int x = 0; x < PARTS; ++x) {
-          if (BK == 2 && __any_sync(0xffffffffu, (sw[x] & 0xffffu) > MAX_DOUBLED || (sw[x] >> 16) > MAX_DOUBLED)) {
-            large |= 1u << x;
-            sw[x] = zw[x] = 0u;
-          }
           // (rows rz + 2 x and the one after it: bits of a row's number are exclusive-ored into the place of its pieces)
           const uint32_t to_z = ((dst + params_off) ^ (32u * x)) + 256u * x, to_s = (to_z ^ 16u) + 128u;
           sts16(to_z, zw[x] & 0xffffu);
@@ -579,40 +609,51 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         for (int x = 0; x < PARTS; ++x) {
           const uint32_t src = raw + code_off + x * (32 * Ly::KROW);
           const uint32_t d0 = dst + row_off + 4096u * x, d1 = d0 ^ 16u, s_row = ((dst + scales_off) ^ (32u * x)) + 256u * x;
-          if (BK == 1 || !((large >> x) & 1u)) {
-            uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
-            load_codes<4, 8 * CB>(src, codes);
-            const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
-            expand_rows<BK, BK - 1, BK - 1, 4>(codes, shift, s0, s1, d0, d1, fields);
+          uint32_t codes[4];  // of eight tokens each (loads first: an access to shared memory does not move past another)
+          load_codes<4, 8 * CB>(src, codes);
+          const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
+          expand_rows<BK, BK - 1, BK - 1, 4>(codes, shift, s0, s1, d0, d1, fields);
+        }
+      } else if (packed) {
+        // Parameters of tokens lane, lane + 32, + 64, + 96, (scale, zero-point); none of tokens that do not exist.  A word of the
+        // operand's rows has tokens (t, t + 2): one of the two lanes writes s and o s, the other z.
+        // (the scales of a token's other channel groups: the warps have to agree on what is in quarters)
+        uint32_t sz[4], top[2] = {0u, 0u};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t at = raw + meta_off + k * (128 * NG);
+          if constexpr (BV == 2 && NG > 1) {
+            uint32_t scales[NG / 2];
+            if constexpr (NG == 4) {
+              const uint2 v = lds64(at);
+              scales[0] = v.x;
+              scales[1] = v.y;
+            } else {
+              scales[0] = lds32(at);
+            }
+            sz[k] = __byte_perm(NG == 4 && vg >= 2 ? scales[NG / 2 - 1] : scales[0], lds16(at + 2 * NG + 2 * vg), vg & 1 ? 0x5432 : 0x5410);
+            if (valid < RB && lane + 32 * k >= valid) sz[k] = scales[0] = scales[NG / 2 - 1] = 0u;
+            top[k >> 1] = __vmaxu2(top[k >> 1], NG == 4 ? __vmaxu2(scales[0], scales[NG / 2 - 1]) : scales[0]);
           } else {
-            const uint32_t group = raw + Ly::RAW_KM + (slot0 + x) * 32 / GS * (4 * D);
-#pragma unroll 1
-            for (int k = 0; k < 8; ++k) {
-              auto s_at = [&](int e) { const int d = 64 * kb + 16 * o + 8 * (k & 1) + e; return group + 2 * (d % 32 * (D / 32) + d / 32); };
-              restore8<BK>(lds32(src + 8 * (k >> 1) * CB) >> (shift + 2 * BK * (k & 1)), s_at, [&](int e) { return s_at(e) + 2 * D; },
-                           (k & 1 ? d1 : d0) + 1024 * (k >> 1));
+            sz[k] = lds16(at + 2 * vg) | lds16(at + 2 * NG + 2 * vg) << 16;
+            if (valid < RB && lane + 32 * k >= valid) sz[k] = 0u;
+            top[k >> 1] = max(top[k >> 1], sz[k] & 0xffffu);
+          }
+        }
+        if constexpr (BV == 2) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (any_large(top[x])) {
+              quarter |= 1u << x;
+              sz[2 * x] = hmul2(sz[2 * x], QUARTERS);
+              sz[2 * x + 1] = hmul2(sz[2 * x + 1], QUARTERS);
             }
           }
         }
-      } else if (packed) {
-        const int valid = n_q - (t_lo + i) * RB;  // tokens of the batch that exist
-        // Parameters of tokens lane, lane + 32, + 64, + 96, (scale, zero-point); none of tokens that do not exist.  A word of the
-        // operand's rows has tokens (t, t + 2): one of the two lanes writes s and o s, the other z.
-        uint32_t sz[4], large = 0u;  // bit x: of half x
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sz[k] = lds16(raw + meta_off + k * (128 * NG)) | lds16(raw + meta_off + k * (128 * NG) + 2 * NG) << 16;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (valid < RB && lane + 32 * k >= valid) sz[k] = 0u;
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          if (BV == 2 && __any_sync(0xffffffffu, (sz[2 * x] & 0xffffu) > MAX_DOUBLED || (sz[2 * x + 1] & 0xffffu) > MAX_DOUBLED)) large |= 1u << x;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t other = __shfl_xor_sync(0xffffffffu, sz[k], 2), first = lane & 2 ? other : sz[k], second = lane & 2 ? sz[k] : other;
           uint32_t s2 = __byte_perm(first, second, 0x5410), z2 = __byte_perm(first, second, 0x7632);
-          if ((large >> (k >> 1)) & 1u) s2 = z2 = 0u;
           const uint32_t to = (dst + params_off + (k >> 1) * Ly::VBLOCK) ^ (64u * (k & 1));
           uint32_t os = BV == 2 ? (lane & 1 ? hadd2(s2, s2) : s2) : (lane & 1 ? s2 : 0u);
           if constexpr (F16) {  // z and o s as the rounding of their sum and what it left off (D. E. Knuth's two-sum: exact)
@@ -629,20 +670,10 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
         for (int x = 0; x < 2; ++x) {
           const uint32_t src = raw + code_off + x * (BV == 2 ? D * 16 : 8), block = dst + x * Ly::VBLOCK;
           const uint32_t d0 = block + row_off, d1 = d0 ^ 16u, s_row = block + scales_off;
-          if (BV == 1 || !((large >> x) & 1u)) {
-            uint32_t codes[STEPS];
-            load_codes<STEPS, 128>(src, codes);
-            const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
-            expand_rows<BV, BV - 1, BV, STEPS>(codes, shift, s0, s1, d0, d1, fields);
-          } else {
-            // (a token that does not exist stands for the last one that does: its numerator is zero)
-#pragma unroll 1
-            for (int k = 0; k < 2 * STEPS; ++k) {
-              auto s_at = [&](int e) { return raw + Ly::RAW_VM + min(64 * x + 16 * o + 8 * (k & 1) + e, valid - 1) * (4 * NG) + 2 * vg; };
-              restore8<BV>(lds32(src + 128 * (k >> 1)) >> (shift + 2 * BV * (k & 1)), s_at, [&](int e) { return s_at(e) + 2 * NG; },
-                           (k & 1 ? d1 : d0) + 1024 * (k >> 1));
-            }
-          }
+          uint32_t codes[STEPS];
+          load_codes<STEPS, 128>(src, codes);
+          const uint4 s0 = lds128(s_row), s1 = lds128(s_row ^ 16u);
+          expand_rows<BV, BV - 1, BV, STEPS>(codes, shift, s0, s1, d0, d1, fields);
         }
       } else {
         // a window batch: the warps of a kind settle its exponent, then write it
@@ -698,6 +729,13 @@ __global__ void __launch_bounds__(R_THREADS, 1) rows_kernel(const __grid_constan
           }
         }
       }
+      if constexpr (BV == 2) {
+        if (!keys && ew < 2 && (quarter >> ew & 1u) != (quarter_ones >> b & 1u)) {
+          quarter_ones ^= 1u << b;
+          write_ones(b, quarter >> ew & 1u ? QUARTERS : 0x3c003c00u);
+        }
+      }
+      if ((keys ? BK : BV) == 2 && ew == 0 && lane == 0) quarter_sm[keys ? 0 : 1][b] = quarter;
       proxy_fence();
       __syncwarp();
       arrive_if(lane == 0, (keys ? bar_kfull : bar_vfull) + 8 * b);

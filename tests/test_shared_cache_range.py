@@ -146,3 +146,49 @@ def test_long_windows_in_half_precision(shape):
     o32, o16 = cache.cross_attention(1, q.to(DEV), f32=True), cache.cross_attention(1, q.to(DEV))
     _compare(cfg, o32, o16, q, lambda b, h: _restored(cfg, K, V, 1, b, h), 1024, [0, 1], [0, 1], True, tokens=[0, 31, 59])
     cache.check_device()
+
+
+# ---- scales that are too large to be doubled in half precision ----
+
+def _wide(x, bits, f16, of_tokens, seed, g=32):
+    """Every third group of x's tensors (g tokens of a channel, or a token's g channels) spread over all that a scale can span: to
+    both ends of half precision for inputs of that type, else 3 (1-bit: 1) times a scale of 62000."""
+    rng = np.random.default_rng(seed)
+    lo, hi = (-65504.0, 65504.0) if f16 and bits == 2 else (-60000.0, 126000.0) if bits == 2 else (-30000.0, 32000.0)
+    B, H, S, D = x[0].shape
+    groups = (B, H, -(-S // g), D) if of_tokens else (B, H, S, D // g)
+    pick = torch.from_numpy(rng.random(groups) < 1 / 3)
+    pick = pick.repeat_interleave(g, 2)[:, :, :S] if of_tokens else pick.repeat_interleave(g, 3)
+    ends = torch.from_numpy(np.where(rng.random(x[0].shape) < 0.5, lo, hi).astype(np.float32))
+    inner = torch.from_numpy(rng.uniform(lo, hi, x[0].shape).astype(np.float32))
+    wide = torch.where(torch.from_numpy(rng.random(x[0].shape) < 0.5), ends, inner).to(x[0].dtype)
+    return [torch.where(pick, wide, t) for t in x]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("T", [1, 17, 1300])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[2], SHAPES[3], SHAPES[6], (64, 4, 1, 64, 64, 2, 2, False),
+                                   (128, 4, 1, 64, 64, 2, 2, True)])
+@pytest.mark.parametrize("which", ["keys", "values"])
+def test_packed_elements_beyond_half_precision(shape, which, T, kernel):
+    D, Hq, Hkv, g, R, kq, vq, f16 = shape
+    S = 700
+    cfg = _shape(shape, batch=2, max_seq=S, kernel=kernel)
+    K, V = _tokens(cfg, 1, S, outliers=False)
+    q = _queries(cfg, 3, T)
+    if which == "keys":
+        K = _wide(K, 2 if kq else 1, f16, True, 4, g)
+        q = (q.float() * 2.0 ** -13).to(q.dtype)  # logits of ordinary size
+    else:
+        V = _wide(V, 2 if vq else 1, f16, False, 5, g)
+    cache = _filled(cfg, K, V)
+    n = [S, 333]
+    lengths = torch.tensor(n, dtype=torch.int32, device=DEV)
+    pairs = f16 and T * cfg.n_q_heads // cfg.n_kv_heads > 128
+    for layer in (0, 1):
+        o32, o16 = (cache.cross_attention(layer, q.to(DEV), lengths=lengths, f32=f32) for f32 in (True, False))
+        for b in (0, 1):
+            _compare(cfg, o32, o16, q, lambda b, h: [x[:n[b]] for x in _restored(cfg, K, V, layer, b, h)],
+                     min(n[b], S - (S - 1) % R - 1), range(Hkv), [b], pairs, products=4, tokens=[0, T - 1])
+    cache.check_device()
