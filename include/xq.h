@@ -320,9 +320,9 @@ int xq_decode_attention_static(xq_cache* c, int layer, const void* q, void* out,
 int xq_decode_step(xq_cache* c, const void* K_new, const void* V_new, const void* q, void* out,
                    const int32_t* layer_order, int mem, void* stream);
 
-/* Waits for `stream` and reports whether a kernel launched through this handle
- * gave up one of its bounded waits or met an index out of range (XQ_ERR_DEVICE; the outputs of that call are
- * then invalid and the handle should be reset) -- every wait inside the kernels
+/* Waits for `stream` and reports whether a kernel launched through this handle, by a call or by a graph that holds
+ * one, gave up one of its bounded waits or met an index out of range (XQ_ERR_DEVICE; the outputs of that call are
+ * then invalid and the handle should be reset, until which it is reported) -- every wait inside the kernels
  * has an iteration limit instead of the ability to hang the GPU.  XQ_OK otherwise.
  * Synchronizes; not for the hot path. */
 int xq_check_device(xq_cache* c, void* stream);

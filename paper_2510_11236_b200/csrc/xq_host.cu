@@ -6,6 +6,8 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
+#include <chrono>
 #include <new>
 #include <vector>
 
@@ -112,7 +114,7 @@ void make_plan(const xq_config* c, Plan& pl) {
   pl.part_acc = take((size_t)dm.B * dm.Hq * XQ_MAX_SPLITS * dm.D * 4);
   pl.part_ml = take((size_t)dm.B * dm.Hq * XQ_MAX_SPLITS * 2 * 4);
   pl.tickets = take(BH * DECODE_MAX_LAYERS * 4);
-  pl.status = take(4);
+  pl.status = take(sizeof(HandleState));
   pl.delta = take((size_t)c->n_layers * 2 * 4 * 8);  // per layer and cache kind: elements by code difference 0..3
   pl.staging_kv_bytes = (size_t)c->n_layers * BH * dm.D * 2;
   pl.staging_q_bytes = (size_t)c->n_layers * dm.B * dm.Hq * dm.D * 2;
@@ -171,7 +173,9 @@ struct xq_cache {
   int sm_count;
   int device;            // CUDA device the handle was created on (-1: none)
   uint8_t* static_base;  // device address of the library's static scratch array on that device (null: not resolved)
-  bool tickets_clean;  // the ticket counters have been zeroed on a stream
+  bool tickets_clean;  // the ticket counters and the status word have been cleared on a stream, not only in a capture
+  unsigned long long capture;            // the latest capture that holds their clearing (0: none)
+  unsigned long long mark, first_mark;   // the mark of their clearing; that of the first one since xq_create or xq_reset
   bool delta_clean;    // the code-difference counters have been zeroed on a stream
   std::vector<uint8_t> repacked;  // per layer: codes or parameters it reads were written since its last decode
   MmaKernels mma_kernels[2][2];  // by (key bits - 1, value bits - 1)
@@ -547,19 +551,42 @@ Scratch workspace_scratch(const xq_cache* c) {
   return s;
 }
 
-// The ticket counters and the status word start at zero: cleared once per handle on the first stream used.
+// A number that no other handle of this or another process is likely to have (G. L. Steele, D. Lea, C. H. Flood, "Fast splittable
+// pseudorandom number generators", 2014: the output function of SplitMix, of a count, the time and an address).
+unsigned long long new_mark(const void* handle) {
+  static std::atomic<unsigned long long> count{0};
+  const auto now = std::chrono::steady_clock::now().time_since_epoch().count();
+  unsigned long long x = (unsigned long long)now + 0x9e3779b97f4a7c15ull * (++count) + ((unsigned long long)(uintptr_t)handle << 20);
+  x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;
+  x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+  return x ^ (x >> 31);
+}
+
+// The ticket counters and the status word start at zero: cleared once per handle on the first stream used.  A call that is
+// captured clears them when its graph runs, which may be never, so the next one outside of the capture clears them too; a
+// clearing that comes after one of the same mark does nothing.
 int ensure_clean_scratch(xq_cache* c, cudaStream_t st) {
   if (c->tickets_clean) return XQ_OK;
-  const Dims& dm = c->plan.dm;
-  cudaError_t e = cudaMemsetAsync(c->ws + c->plan.tickets, 0, (size_t)dm.B * dm.Hkv * DECODE_MAX_LAYERS * 4, st);
-  if (e == cudaSuccess) e = cudaMemsetAsync(c->ws + c->plan.status, 0, 4, st);
-  if (e != cudaSuccess) return fail_cuda(c, e);
-  // (a call that is captured clears them when its graph runs, which may be never: the next one clears them too)
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-  e = cudaStreamIsCapturing(st, &capture);
+  unsigned long long id = 0;
+  cudaError_t e = cudaStreamGetCaptureInfo(st, &capture, &id);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  c->tickets_clean = capture == cudaStreamCaptureStatusNone;
+  const bool captured = capture != cudaStreamCaptureStatusNone;
+  if (captured && c->capture == id) return XQ_OK;
+  const Dims& dm = c->plan.dm;
+  e = launch_clear((HandleState*)(c->ws + c->plan.status), c->mark, (unsigned int*)(c->ws + c->plan.tickets),
+                   (size_t)dm.B * dm.Hkv * DECODE_MAX_LAYERS, st);
+  if (e != cudaSuccess) return fail_cuda(c, e);
+  if (captured) c->capture = id;
+  else c->tickets_clean = true;
   return XQ_OK;
+}
+
+// The counters may be anything: the next call clears them.
+void dirty_scratch(xq_cache* c) {
+  c->tickets_clean = false;
+  c->capture = 0;
+  ++c->mark;
 }
 
 // Merged code of (e0, e1) for every pair of B-bit codes, at bits 2 * (4 e0 + e1): round(gamma_0 e0 + gamma_1 e1) in
@@ -660,7 +687,7 @@ int decode_impl(xq_cache* c, int layer, const void* q, void* out, int out_f32, c
   }
   rc = launch_decode(c, p, use_mma, workspace_scratch(c), st);
   if (rc != XQ_OK) {
-    if (use_mma) c->tickets_clean = false;
+    if (use_mma) dirty_scratch(c);
     return rc;
   }
   if (use_mma) c->repacked[layer] = 0;
@@ -755,7 +782,7 @@ int decode_layers(xq_cache* c, const int* order, int n, const uint8_t* q, uint8_
     p.late_wait = i > 0;
     rc = launch_decode(c, p, true, workspace_scratch(c), st);
     if (rc != XQ_OK) {
-      c->tickets_clean = false;
+      dirty_scratch(c);
       return rc;
     }
     if (p.paired) c->pair_layers += p.n_layers;
@@ -811,6 +838,8 @@ int xq_create(const xq_config* cfg, void* dev_workspace, size_t bytes, xq_cache*
   c->used = 0;
   c->sm_count = 148;
   c->tickets_clean = false;
+  c->capture = 0;
+  c->mark = c->first_mark = new_mark(c);
   c->delta_clean = false;
   c->device = -1;
   c->static_base = nullptr;
@@ -847,7 +876,8 @@ int xq_reset(xq_cache* c) {
   if (!c) return XQ_ERR_ARG;
   for (auto& s : c->seq) s = 0;
   for (auto& r : c->repacked) r = 1;  // as after xq_create: the first decode of a layer waits for its predecessor
-  c->tickets_clean = false;           // tickets and status are cleared again before their next use
+  dirty_scratch(c);                   // tickets and status are cleared again before their next use
+  c->first_mark = c->mark;
   c->delta_clean = false;             // and so are the code-difference counters
   return XQ_OK;
 }
@@ -973,7 +1003,7 @@ int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int ou
   }
   c->launches++;
   if (e != cudaSuccess) {
-    c->tickets_clean = false;
+    dirty_scratch(c);
     return fail_cuda(c, e);
   }
   c->repacked[layer] = 0;  // the launch began after everything before it in the stream had completed
@@ -1205,7 +1235,7 @@ int launch_shared_decode(xq_cache* c, const xq_cache* kv, int layer, const RowsP
     p.early_fetch = p.late_wait = j > 0 || first_chained;  // what this launch reads was complete when the first one had waited
     const int rc = launch_decode(c, p, true, workspace_scratch(c), st);
     if (rc != XQ_OK) {
-      c->tickets_clean = false;
+      dirty_scratch(c);
       return rc;
     }
   }
@@ -1534,11 +1564,12 @@ int xq_check_device(xq_cache* c, void* stream) {
   if (!c) return XQ_ERR_ARG;
   cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  if (!c->tickets_clean) return XQ_OK;  // the status word has not been used yet
-  int status = 0;
-  e = cudaMemcpy(&status, c->ws + c->plan.status, 4, cudaMemcpyDeviceToHost);
+  if (!c->tickets_clean && !c->capture && c->mark == c->first_mark) return XQ_OK;  // the status word has not been used yet
+  HandleState state;
+  e = cudaMemcpy(&state, c->ws + c->plan.status, sizeof(state), cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  return status ? XQ_ERR_DEVICE : XQ_OK;
+  // (no call since xq_create or xq_reset has run: another mark, and the status means nothing)
+  return state.mark - c->first_mark <= 0xffffffffull && state.status ? XQ_ERR_DEVICE : XQ_OK;
 }
 
 int xq_delta_histogram(xq_cache* c, int layer, int kind, unsigned long long counts[4], void* stream) {

@@ -1,0 +1,103 @@
+"""Calls that a CUDA graph holds, the first ones of their handle among them: what they report, and what later calls may take for
+granted."""
+import pytest
+import torch
+
+import paper_2510_11236_b200 as xq
+from tests.test_shared_cache import DEV, _config, _filled, _queries, _tokens
+
+
+def _reports(cache):
+    try:
+        cache.check_device()
+    except xq.XQError as e:
+        assert e.code == xq.XQ_ERR_DEVICE
+        return True
+    return False
+
+
+def _gather_then_decode(index):
+    """A handle whose first calls are captured: a gather, then a decode of both layers and a cross attention."""
+    cfg = _config(batch=4, max_seq=300)
+    src, dst = _filled(cfg, *_tokens(cfg, 1, 200)), xq.Cache(cfg, DEV)
+    dst.workspace.fill_(0xff)
+    q = _queries(cfg, 2, 1).to(DEV)
+    outs = [torch.empty_like(q[0]), torch.empty_like(q[0]), torch.empty_like(q)]
+    space = torch.empty(xq.xq_cross_workspace_bytes(dst.handle, 1), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dst.gather_sequences(src, index)
+        for layer in (0, 1):
+            dst.decode_attention(layer, q[0], out=outs[layer])
+        dst.cross_attention(1, q, out=outs[2], workspace=space)
+    want = [src.decode_attention(0, q[0]), src.decode_attention(1, q[0]), src.cross_attention(1, q)]
+    return src, dst, q, outs, want, graph
+
+
+@pytest.mark.gpu
+def test_a_later_call_of_the_graph_does_not_hide_a_report():
+    index = torch.tensor([0, 1, -1, 3], dtype=torch.int32, device=DEV)
+    src, dst, q, outs, want, graph = _gather_then_decode(index)
+    assert not _reports(dst)  # the graph has not run
+    graph.replay()
+    assert _reports(dst)
+    # nor does the next run of the graph, until the handle is reset
+    index.copy_(torch.arange(4, dtype=torch.int32))
+    graph.replay()
+    assert _reports(dst)
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    xq.xq_reset(dst.handle)
+    assert not _reports(dst)
+    dst.gather_sequences(src, index)
+    assert not _reports(dst) and torch.equal(dst.decode_attention(1, q[0]), want[1])
+
+
+@pytest.mark.gpu
+def test_an_eager_call_does_not_hide_what_a_graph_reported():
+    index = torch.tensor([0, 9, 2, 3], dtype=torch.int32, device=DEV)
+    src, dst, q, outs, want, graph = _gather_then_decode(index)
+    graph.replay()
+    dst.cross_attention(0, q)  # the handle's first call outside of a graph
+    assert _reports(dst)
+
+
+@pytest.mark.gpu
+def test_graph_of_first_calls_gives_the_results_of_the_others():
+    index = torch.arange(4, dtype=torch.int32, device=DEV)
+    src, dst, q, outs, want, graph = _gather_then_decode(index)
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert not _reports(dst)
+
+
+def _nodes(calls):
+    runtime = pytest.importorskip("cuda.bindings.runtime")
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        calls()
+    err, _, n = runtime.cudaGraphGetNodes(runtime.cudaGraph_t(graph.raw_cuda_graph()), 0)
+    assert int(err) == 0
+    return n
+
+
+@pytest.mark.gpu
+def test_a_graph_clears_the_counters_once():
+    # what clears them stands between launches that overlap: at most two nodes before the first call, none before the others
+    cfg = _config(batch=2, max_seq=600)
+    q = _queries(cfg, 2, 3).to(DEV)
+    out = torch.empty_like(q)
+
+    def calls(cache):
+        for _ in range(3):
+            for layer in (0, 1):
+                cache.decode_attention(layer, q[0], out=out[0])
+                cache.attention_chunk(layer, q, out=out)
+    fresh, used = (_filled(cfg, *_tokens(cfg, 1, 500)) for _ in range(2))
+    calls(used)
+    torch.cuda.synchronize()
+    n = _nodes(lambda: calls(used))
+    assert n >= 12 and _nodes(lambda: calls(fresh)) <= n + 2
