@@ -173,10 +173,9 @@ struct xq_cache {
   int sm_count;
   int device;            // CUDA device the handle was created on (-1: none)
   uint8_t* static_base;  // device address of the library's static scratch array on that device (null: not resolved)
-  bool tickets_clean;  // the ticket counters and the status word have been cleared on a stream, not only in a capture
+  bool tickets_clean;  // the counters (tickets, status, code differences) have been cleared on a stream, not only in a capture
   unsigned long long capture;            // the latest capture that holds their clearing (0: none)
   unsigned long long mark, first_mark;   // the mark of their clearing; that of the first one since xq_create or xq_reset
-  bool delta_clean;    // the code-difference counters have been zeroed on a stream
   std::vector<uint8_t> repacked;  // per layer: codes or parameters it reads were written since its last decode
   MmaKernels mma_kernels[2][2];  // by (key bits - 1, value bits - 1)
   MmaPlan mma_plan[2][2];    // and the splits of the latest number of batches asked for; batches 0 = none yet
@@ -562,7 +561,7 @@ unsigned long long new_mark(const void* handle) {
   return x ^ (x >> 31);
 }
 
-// The ticket counters and the status word start at zero: cleared once per handle on the first stream used.  A call that is
+// The ticket counters, those of code differences and the status word start at zero: cleared once per handle on the first stream used.  A call that is
 // captured clears them when its graph runs, which may be never, so the next one outside of the capture clears them too; a
 // clearing that comes after one of the same mark does nothing.
 int ensure_clean_scratch(xq_cache* c, cudaStream_t st) {
@@ -575,7 +574,7 @@ int ensure_clean_scratch(xq_cache* c, cudaStream_t st) {
   if (captured && c->capture == id) return XQ_OK;
   const Dims& dm = c->plan.dm;
   e = launch_clear((HandleState*)(c->ws + c->plan.status), c->mark, (unsigned int*)(c->ws + c->plan.tickets),
-                   (size_t)dm.B * dm.Hkv * DECODE_MAX_LAYERS, st);
+                   (size_t)dm.B * dm.Hkv * DECODE_MAX_LAYERS, (unsigned long long*)(c->ws + c->plan.delta), (size_t)c->cfg.n_layers * 2 * 4, st);
   if (e != cudaSuccess) return fail_cuda(c, e);
   if (captured) c->capture = id;
   else c->tickets_clean = true;
@@ -643,12 +642,11 @@ int pack_layers(xq_cache* c, const int* layers, int n, const void* K, const void
     pl.eta_k = pl.L.bk == 1 ? c->cfg.eta1 : c->cfg.eta2;
     pl.eta_v = pl.L.bv == 1 ? c->cfg.eta1 : c->cfg.eta2;
   }
-  cudaError_t e;
-  if (c->cfg.delta_stats && !c->delta_clean) {
-    e = cudaMemsetAsync(c->ws + c->plan.delta, 0, (size_t)c->cfg.n_layers * 2 * 4 * 8, st);
-    if (e != cudaSuccess) return fail_cuda(c, e);
-    c->delta_clean = true;
+  if (c->cfg.delta_stats) {
+    const int rc = ensure_clean_scratch(c, st);
+    if (rc != XQ_OK) return rc;
   }
+  cudaError_t e;
   {
     Timer t(c, st, 2);
     e = launch_pack(p, st);
@@ -840,7 +838,6 @@ int xq_create(const xq_config* cfg, void* dev_workspace, size_t bytes, xq_cache*
   c->tickets_clean = false;
   c->capture = 0;
   c->mark = c->first_mark = new_mark(c);
-  c->delta_clean = false;
   c->device = -1;
   c->static_base = nullptr;
   memset(c->mma_kernels, 0, sizeof(c->mma_kernels));
@@ -876,9 +873,8 @@ int xq_reset(xq_cache* c) {
   if (!c) return XQ_ERR_ARG;
   for (auto& s : c->seq) s = 0;
   for (auto& r : c->repacked) r = 1;  // as after xq_create: the first decode of a layer waits for its predecessor
-  dirty_scratch(c);                   // tickets and status are cleared again before their next use
+  dirty_scratch(c);                   // the counters are cleared again before their next use
   c->first_mark = c->mark;
-  c->delta_clean = false;             // and so are the code-difference counters
   return XQ_OK;
 }
 
@@ -1560,16 +1556,28 @@ int xq_decode_step(xq_cache* c, const void* K_new, const void* V_new, const void
   return XQ_OK;
 }
 
-int xq_check_device(xq_cache* c, void* stream) {
-  if (!c) return XQ_ERR_ARG;
+namespace {
+// The handle's counters as the stream has left them; counted: they have been cleared since xq_create or xq_reset, else they mean
+// nothing.
+int read_state(xq_cache* c, void* stream, HandleState& state, bool& counted) {
+  counted = false;
   cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  if (!c->tickets_clean && !c->capture && c->mark == c->first_mark) return XQ_OK;  // the status word has not been used yet
-  HandleState state;
+  if (!c->tickets_clean && !c->capture && c->mark == c->first_mark) return XQ_OK;  // no call has used them
   e = cudaMemcpy(&state, c->ws + c->plan.status, sizeof(state), cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  // (no call since xq_create or xq_reset has run: another mark, and the status means nothing)
-  return state.mark - c->first_mark <= 0xffffffffull && state.status ? XQ_ERR_DEVICE : XQ_OK;
+  counted = state.mark - c->first_mark <= 0xffffffffull;
+  return XQ_OK;
+}
+}  // namespace
+
+int xq_check_device(xq_cache* c, void* stream) {
+  if (!c) return XQ_ERR_ARG;
+  HandleState state;
+  bool counted;
+  const int rc = read_state(c, stream, state, counted);
+  if (rc != XQ_OK) return rc;
+  return counted && state.status ? XQ_ERR_DEVICE : XQ_OK;
 }
 
 int xq_delta_histogram(xq_cache* c, int layer, int kind, unsigned long long counts[4], void* stream) {
@@ -1577,10 +1585,11 @@ int xq_delta_histogram(xq_cache* c, int layer, int kind, unsigned long long coun
   if (layer < 0 || layer >= c->cfg.n_layers || kind < 0 || kind > 1) return XQ_ERR_ARG;
   if (!c->cfg.delta_stats) return XQ_ERR_CONFIG;
   for (int k = 0; k < 4; ++k) counts[k] = 0ull;
-  cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
-  if (e != cudaSuccess) return fail_cuda(c, e);
-  if (!c->delta_clean) return XQ_OK;  // nothing has been counted yet
-  e = cudaMemcpy(counts, c->ws + c->plan.delta + (size_t)(layer * 2 + kind) * 4 * 8, 4 * 8, cudaMemcpyDeviceToHost);
+  HandleState state;
+  bool counted;
+  const int rc = read_state(c, stream, state, counted);
+  if (rc != XQ_OK || !counted) return rc;
+  const cudaError_t e = cudaMemcpy(counts, c->ws + c->plan.delta + (size_t)(layer * 2 + kind) * 4 * 8, 4 * 8, cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return fail_cuda(c, e);
   return XQ_OK;
 }

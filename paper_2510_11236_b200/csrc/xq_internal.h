@@ -89,7 +89,7 @@ struct DecodeLayer {
 struct HandleState {
   int status;               // set by a kernel that gave up a bounded wait or met a bad index
   int unused;
-  unsigned long long mark;  // which clearing of the tickets and of the status was the last one to take effect
+  unsigned long long mark;  // which clearing of the counters was the last one to take effect
 };
 
 constexpr int DECODE_MAX_LAYERS = 32;  // layers one launch can take (of equal lengths and bit-widths)
@@ -263,9 +263,10 @@ cudaError_t launch_dependent(void (*kernel)(P), dim3 grid, dim3 block, size_t sm
 }
 #endif
 
-// Clears the n tickets and the status unless the state's mark is `mark` or a later one: recorded in a graph, it takes effect when the
-// graph runs, whatever has run by then, and hides no status.
-cudaError_t launch_clear(HandleState* state, unsigned long long mark, unsigned int* tickets, size_t n, cudaStream_t st);
+// Clears the n tickets, the n_delta counters of code differences and the status unless the state's mark is `mark` or a later one:
+// recorded in a graph, it takes effect when the graph runs, whatever has run by then, and hides no status.
+cudaError_t launch_clear(HandleState* state, unsigned long long mark, unsigned int* tickets, size_t n, unsigned long long* delta, size_t n_delta,
+                         cudaStream_t st);
 cudaError_t launch_pack(const PackParams& p, cudaStream_t st);
 cudaError_t launch_window_append(const WindowParams& p, cudaStream_t st);
 cudaError_t launch_decode_generic(const DecodeParams& p, cudaStream_t st);

@@ -1,4 +1,4 @@
-// The counters of a handle that start at zero (merge tickets, status word), and the mark that says so.
+// The counters of a handle that start at zero (merge tickets, status word, code differences), and the mark that says so.
 #include <algorithm>
 
 #include "xq_internal.h"
@@ -14,9 +14,12 @@ __device__ __forceinline__ bool marked(const HandleState* state, unsigned long l
   return state->mark - mark <= 0xffffffffull;
 }
 
-__global__ void __launch_bounds__(CLEAR_THREADS) clear_kernel(const HandleState* state, unsigned long long mark, unsigned int* tickets, size_t n) {
+__global__ void __launch_bounds__(CLEAR_THREADS) clear_kernel(const HandleState* state, unsigned long long mark, unsigned int* tickets, size_t n,
+                                                              unsigned long long* delta, size_t n_delta) {
   if (marked(state, mark)) return;
-  for (size_t i = (size_t)blockIdx.x * CLEAR_THREADS + threadIdx.x; i < n; i += (size_t)gridDim.x * CLEAR_THREADS) tickets[i] = 0u;
+  const size_t first = (size_t)blockIdx.x * CLEAR_THREADS + threadIdx.x, step = (size_t)gridDim.x * CLEAR_THREADS;
+  for (size_t i = first; i < n; i += step) tickets[i] = 0u;
+  for (size_t i = first; i < n_delta; i += step) delta[i] = 0ull;
 }
 
 __global__ void mark_kernel(HandleState* state, unsigned long long mark) {
@@ -27,9 +30,10 @@ __global__ void mark_kernel(HandleState* state, unsigned long long mark) {
 
 }  // namespace
 
-cudaError_t launch_clear(HandleState* state, unsigned long long mark, unsigned int* tickets, size_t n, cudaStream_t st) {
+cudaError_t launch_clear(HandleState* state, unsigned long long mark, unsigned int* tickets, size_t n, unsigned long long* delta, size_t n_delta,
+                         cudaStream_t st) {
   const unsigned ctas = (unsigned)std::min<size_t>((n + CLEAR_THREADS - 1) / CLEAR_THREADS, 592);
-  clear_kernel<<<std::max(1u, ctas), CLEAR_THREADS, 0, st>>>(state, mark, tickets, n);
+  clear_kernel<<<std::max(1u, ctas), CLEAR_THREADS, 0, st>>>(state, mark, tickets, n, delta, n_delta);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   mark_kernel<<<1, 1, 0, st>>>(state, mark);  // (a kernel of its own: a block of the other one may begin after all others)

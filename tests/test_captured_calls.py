@@ -101,3 +101,49 @@ def test_a_graph_clears_the_counters_once():
     torch.cuda.synchronize()
     n = _nodes(lambda: calls(used))
     assert n >= 12 and _nodes(lambda: calls(fresh)) <= n + 2
+
+
+@pytest.mark.gpu
+def test_code_differences_after_a_capture_that_never_runs():
+    # the counters of xq_delta_histogram start at zero, whatever the first append that counts was captured into
+    cfg = _config(batch=2, max_seq=300, delta_stats=1)
+    K, V = _tokens(cfg, 1, 200)
+    want, fresh = xq.Cache(cfg, DEV), xq.Cache(cfg, DEV)
+    fresh.workspace.fill_(0xff)
+    torch.cuda.synchronize()
+    k, v = ([x.to(DEV) for x in y] for y in (K, V))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for layer in (0, 1):
+            fresh.append_kv(layer, k[layer], v[layer])
+    stream = torch.cuda.current_stream().cuda_stream
+    assert xq.xq_delta_histogram(fresh.handle, 1, 0, stream) == (0, [0, 0, 0, 0])
+    xq.xq_reset(fresh.handle)
+    for cache in (want, fresh):
+        for layer in (0, 1):
+            cache.append_kv(layer, k[layer], v[layer])
+    for kind in (0, 1):
+        rc, counts = xq.xq_delta_histogram(want.handle, 1, kind, stream)
+        assert rc == 0 and sum(counts) == 2 * 2 * 192 * 128
+        assert xq.xq_delta_histogram(fresh.handle, 1, kind, stream) == (0, counts)
+
+
+@pytest.mark.gpu
+def test_code_differences_that_a_graph_counts():
+    cfg = _config(batch=2, max_seq=300, delta_stats=1)
+    K, V = _tokens(cfg, 1, 200)
+    k, v = ([x.to(DEV) for x in y] for y in (K, V))
+    want = _filled(cfg, K, V)
+    fresh = xq.Cache(cfg, DEV)
+    fresh.workspace.fill_(0xff)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for layer in (0, 1):
+            fresh.append_kv(layer, k[layer], v[layer])
+    graph.replay()
+    stream = torch.cuda.current_stream().cuda_stream
+    once = xq.xq_delta_histogram(want.handle, 1, 0, stream)
+    assert xq.xq_delta_histogram(fresh.handle, 1, 0, stream) == once
+    graph.replay()  # counts once more
+    assert xq.xq_delta_histogram(fresh.handle, 1, 0, stream) == (0, [2 * n for n in once[1]])
