@@ -176,7 +176,10 @@ struct xq_cache {
   bool tickets_clean;  // the counters (tickets, status, code differences) have been cleared on a stream, not only in a capture
   unsigned long long capture;            // the latest capture that holds their clearing (0: none)
   unsigned long long mark, first_mark;   // the mark of their clearing; that of the first one since xq_create or xq_reset
-  std::vector<uint8_t> repacked;  // per layer: codes or parameters it reads were written since its last decode
+  // per layer: codes or parameters it reads were written since its last decode (1), or by a captured call, whose graph may run
+  // at any time (2); and since its last decode in the capture `flags_capture`
+  std::vector<uint8_t> repacked, repacked_captured;
+  unsigned long long flags_capture;
   MmaKernels mma_kernels[2][2];  // by (key bits - 1, value bits - 1)
   MmaPlan mma_plan[2][2];    // and the splits of the latest number of batches asked for; batches 0 = none yet
   MmaPlan shared_plan;       // the same of calls whose rows read one cache, and what it was made for
@@ -561,22 +564,55 @@ unsigned long long new_mark(const void* handle) {
   return x ^ (x >> 31);
 }
 
+// The capture that `st` is part of, 0: none.
+int capture_of(xq_cache* c, cudaStream_t st, unsigned long long& id) {
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  id = 0;
+  const cudaError_t e = cudaStreamGetCaptureInfo(st, &capture, &id);
+  if (e != cudaSuccess) return fail_cuda(c, e);
+  if (capture == cudaStreamCaptureStatusNone) id = 0;
+  return XQ_OK;
+}
+
+// Whether a layer's packed data may have been written by the launches just before a call, and that it has been (written) or
+// cannot have been any more (read, by a call that waits for them or did not have to).  A captured call's reading counts for its
+// capture alone: the graph may never run.
+std::vector<uint8_t>& flags_of(xq_cache* c, unsigned long long capture) {
+  if (!capture) return c->repacked;
+  if (c->flags_capture != capture) {
+    c->flags_capture = capture;
+    for (size_t l = 0; l < c->repacked.size(); ++l) c->repacked_captured[l] = c->repacked[l] != 0;
+  }
+  return c->repacked_captured;
+}
+bool maybe_written(xq_cache* c, int layer, unsigned long long capture) { return flags_of(c, capture)[layer] != 0; }
+void mark_written(xq_cache* c, int layer, unsigned long long capture) {
+  if (capture) {
+    flags_of(c, capture)[layer] = 1;
+    c->repacked[layer] = 2;
+  } else if (c->repacked[layer] == 0) {
+    c->repacked[layer] = 1;
+  }
+}
+void mark_read(xq_cache* c, int layer, unsigned long long capture) {
+  uint8_t& flag = flags_of(c, capture)[layer];
+  if (flag == 1) flag = 0;
+}
+
 // The ticket counters, those of code differences and the status word start at zero: cleared once per handle on the first stream used.  A call that is
 // captured clears them when its graph runs, which may be never, so the next one outside of the capture clears them too; a
 // clearing that comes after one of the same mark does nothing.
 int ensure_clean_scratch(xq_cache* c, cudaStream_t st) {
   if (c->tickets_clean) return XQ_OK;
-  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-  unsigned long long id = 0;
-  cudaError_t e = cudaStreamGetCaptureInfo(st, &capture, &id);
-  if (e != cudaSuccess) return fail_cuda(c, e);
-  const bool captured = capture != cudaStreamCaptureStatusNone;
-  if (captured && c->capture == id) return XQ_OK;
+  unsigned long long capture;
+  const int rc = capture_of(c, st, capture);
+  if (rc != XQ_OK) return rc;
+  if (capture && c->capture == capture) return XQ_OK;
   const Dims& dm = c->plan.dm;
-  e = launch_clear((HandleState*)(c->ws + c->plan.status), c->mark, (unsigned int*)(c->ws + c->plan.tickets),
+  const cudaError_t e = launch_clear((HandleState*)(c->ws + c->plan.status), c->mark, (unsigned int*)(c->ws + c->plan.tickets),
                    (size_t)dm.B * dm.Hkv * DECODE_MAX_LAYERS, (unsigned long long*)(c->ws + c->plan.delta), (size_t)c->cfg.n_layers * 2 * 4, st);
   if (e != cudaSuccess) return fail_cuda(c, e);
-  if (captured) c->capture = id;
+  if (capture) c->capture = capture;
   else c->tickets_clean = true;
   return XQ_OK;
 }
@@ -646,6 +682,9 @@ int pack_layers(xq_cache* c, const int* layers, int n, const void* K, const void
     const int rc = ensure_clean_scratch(c, st);
     if (rc != XQ_OK) return rc;
   }
+  unsigned long long capture;
+  const int rc = capture_of(c, st, capture);
+  if (rc != XQ_OK) return rc;
   cudaError_t e;
   {
     Timer t(c, st, 2);
@@ -658,7 +697,7 @@ int pack_layers(xq_cache* c, const int* layers, int n, const void* K, const void
     for (int l2 = 0; l2 < c->cfg.n_layers; ++l2)
       if (l2 == layers[i] || k_owner(&c->cfg, l2) == layers[i] || v_owner(&c->cfg, l2) == layers[i] ||
           k_owner(&c->cfg, layers[i]) == l2 || v_owner(&c->cfg, layers[i]) == l2)
-        c->repacked[l2] = 1;
+        mark_written(c, l2, capture);
   return XQ_OK;
 }
 
@@ -675,12 +714,14 @@ int decode_impl(xq_cache* c, int layer, const void* q, void* out, int out_f32, c
   int rc = prepare_decode(c, layer, q, out, out_f32, nullptr, nullptr, c->seq[layer], p, use_mma, vis);
   if (rc != XQ_OK) return rc;
   p.lse = lse;
+  unsigned long long capture = 0;
   if (use_mma) {
     rc = ensure_clean_scratch(c, st);
+    if (rc == XQ_OK) rc = capture_of(c, st, capture);
     if (rc != XQ_OK) return rc;
     // the packed streams may be fetched ahead of the preceding kernel unless a pack kernel wrote them since
     // this layer's last decode (then that kernel may be the writer, or only just behind it)
-    p.early_fetch = c->repacked[layer] ? 0 : 1;
+    p.early_fetch = maybe_written(c, layer, capture) ? 0 : 1;
     if (chained) p.early_fetch = p.late_wait = 1;
   }
   rc = launch_decode(c, p, use_mma, workspace_scratch(c), st);
@@ -688,7 +729,7 @@ int decode_impl(xq_cache* c, int layer, const void* q, void* out, int out_f32, c
     if (use_mma) dirty_scratch(c);
     return rc;
   }
-  if (use_mma) c->repacked[layer] = 0;
+  if (use_mma) mark_read(c, layer, capture);
   if (was_mma) *was_mma = use_mma;
   return XQ_OK;
 }
@@ -704,7 +745,9 @@ int decode_layers(xq_cache* c, const int* order, int n, const uint8_t* q, uint8_
                   const uint8_t* V_new, cudaStream_t st) {
   const Dims& dm = c->plan.dm;
   const size_t kv_layer = (size_t)dm.B * dm.Hkv * dm.D * 2, q_layer = (size_t)dm.B * dm.Hq * dm.D * 2;
+  unsigned long long capture = 0;
   int rc = ensure_clean_scratch(c, st);
+  if (rc == XQ_OK) rc = capture_of(c, st, capture);
   if (rc != XQ_OK) return rc;
   const bool joint = n >= MIN_JOINT_LAYERS;
   // Pairs make half as many CTAs that take longer: where all layers one by one fit a wave they would only idle SMs (one
@@ -753,7 +796,7 @@ int decode_layers(xq_cache* c, const int* order, int n, const uint8_t* q, uint8_
     if (!joint) most = 1;
     p.paired = in_pair(i) && most >= 2 && mma_kernels(c, l0).pairs;
     if (p.paired) most -= most % 2;
-    bool packed = c->repacked[l0] != 0;
+    bool packed = maybe_written(c, l0, capture);
     int j = i + 1;
     for (; j < n && j - i < most && c->seq[order[j]] == c->seq[l0] && (!p.paired || in_pair(j)); ++j) {
       const int l = order[j];
@@ -763,7 +806,7 @@ int decode_layers(xq_cache* c, const int* order, int n, const uint8_t* q, uint8_
       p.layer[j - i] = {L, (const uint16_t*)(q + l * q_layer), out + l * q_layer,
                         K_new ? (const uint16_t*)(K_new + l * kv_layer) : nullptr,
                         V_new ? (const uint16_t*)(V_new + l * kv_layer) : nullptr};
-      packed = packed || c->repacked[l] != 0;
+      packed = packed || maybe_written(c, l, capture);
     }
     p.n_layers = j - i;
     // One by one, with many CTAs of some length, the kernel with three CTAs an SM: its tensor memory costs a CTA ~1 us, which
@@ -785,7 +828,7 @@ int decode_layers(xq_cache* c, const int* order, int n, const uint8_t* q, uint8_
     }
     if (p.paired) c->pair_layers += p.n_layers;
     for (; i < j; ++i) {
-      c->repacked[order[i]] = 0;
+      mark_read(c, order[i], capture);
       if (K_new) c->seq[order[i]] += 1;
     }
   }
@@ -821,6 +864,7 @@ int xq_create(const xq_config* cfg, void* dev_workspace, size_t bytes, xq_cache*
     make_plan(cfg, c->plan);
     c->seq.assign(cfg->n_layers, 0);
     c->repacked.assign(cfg->n_layers, 1);
+    c->repacked_captured.assign(cfg->n_layers, 0);
     for (auto* v : {&c->step_len, &c->step_order, &c->step_run}) v->assign(cfg->n_layers, 0);
     for (auto* v : {&c->step_seen, &c->step_paired, &c->step_taken}) v->assign(cfg->n_layers, 0);
   } catch (const std::bad_alloc&) {
@@ -836,7 +880,7 @@ int xq_create(const xq_config* cfg, void* dev_workspace, size_t bytes, xq_cache*
   c->used = 0;
   c->sm_count = 148;
   c->tickets_clean = false;
-  c->capture = 0;
+  c->capture = c->flags_capture = 0;
   c->mark = c->first_mark = new_mark(c);
   c->device = -1;
   c->static_base = nullptr;
@@ -872,7 +916,7 @@ int xq_destroy(xq_cache* c) {
 int xq_reset(xq_cache* c) {
   if (!c) return XQ_ERR_ARG;
   for (auto& s : c->seq) s = 0;
-  for (auto& r : c->repacked) r = 1;  // as after xq_create: the first decode of a layer waits for its predecessor
+  for (auto& r : c->repacked) r = std::max<uint8_t>(r, 1);  // as after xq_create: the first decode of a layer waits for its predecessor
   dirty_scratch(c);                   // the counters are cleared again before their next use
   c->first_mark = c->mark;
   return XQ_OK;
@@ -968,6 +1012,7 @@ bool tokens_one_by_one(const xq_cache* c, int layer, int T) {
 }
 
 int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int out_f32, float* lse, cudaStream_t st) {
+  unsigned long long capture;
   int rc = ensure_clean_scratch(c, st);
   if (rc != XQ_OK) return rc;
   const Dims& dm = c->plan.dm;
@@ -1002,7 +1047,7 @@ int launch_chunk(xq_cache* c, int layer, const void* q, void* out, int T, int ou
     dirty_scratch(c);
     return fail_cuda(c, e);
   }
-  c->repacked[layer] = 0;  // the launch began after everything before it in the stream had completed
+  if (capture_of(c, st, capture) == XQ_OK) mark_read(c, layer, capture);  // the launch began after everything before it in the stream had completed
   return XQ_OK;
 }
 
@@ -1383,7 +1428,9 @@ int xq_gather_sequences(xq_cache* dst, const xq_cache* src, const int32_t* index
   if (dst == src && dst->cfg.batch > gather_place_limit()) return XQ_ERR_CAPACITY;
   if (!on_device(dst) || src->device != dst->device) return XQ_ERR_ARG;
   cudaStream_t st = (cudaStream_t)stream;
-  const int rc = ensure_clean_scratch(dst, st);
+  unsigned long long capture = 0;
+  int rc = ensure_clean_scratch(dst, st);
+  if (rc == XQ_OK) rc = capture_of(dst, st, capture);
   if (rc != XQ_OK) return rc;
   const Dims &ds = src->plan.dm, &dd = dst->plan.dm;
   GatherParams p;
@@ -1425,7 +1472,7 @@ int xq_gather_sequences(xq_cache* dst, const xq_cache* src, const int32_t* index
     if (e != cudaSuccess) return fail_cuda(dst, e);
   }
   for (int l = 0; l < L; ++l) dst->seq[l] = src->seq[l];
-  for (auto& x : dst->repacked) x = 1;  // the next decode of every layer waits for this launch
+  for (int l = 0; l < L; ++l) mark_written(dst, l, capture);  // the next decode of every layer waits for this launch
   return XQ_OK;
 }
 

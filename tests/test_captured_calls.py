@@ -147,3 +147,45 @@ def test_code_differences_that_a_graph_counts():
     assert xq.xq_delta_histogram(fresh.handle, 1, 0, stream) == once
     graph.replay()  # counts once more
     assert xq.xq_delta_histogram(fresh.handle, 1, 0, stream) == (0, [2 * n for n in once[1]])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("writer", ["gather", "append"])
+def test_a_captured_decode_says_nothing_about_calls_outside(writer):
+    # a decode fetches packed data early when it has waited for the launch that wrote them before; one that was only captured
+    # has not.  The writer is held back by other work, and the decode launched right behind it.
+    S = 1500
+    cfg = _config(batch=4, max_seq=4000)
+    src = _filled(cfg, *_tokens(cfg, 1, S))
+    other = _filled(cfg, *_tokens(cfg, 2, S))
+    more = [[x.to(DEV) for x in y] for y in _tokens(cfg, 3, S)]
+    q = _queries(cfg, 4, 1)[0].to(DEV)
+    index = torch.tensor([3, 1, 0, 2], dtype=torch.int32, device=DEV)
+    dst, want = xq.Cache(cfg, DEV), xq.Cache(cfg, DEV)
+    out, side, graphs = torch.empty_like(q), torch.cuda.Stream(), []
+    for k in range(6):
+        for cache in (want, dst):
+            xq.xq_reset(cache.handle)
+            cache.gather_sequences(other, index)  # what an early fetch would find
+            cache.decode_attention(0, q, out=out), cache.decode_attention(1, q, out=out)
+        layer = k % 2
+        for cache in (want, dst):
+            torch.cuda.synchronize()
+            if cache is dst:
+                torch.cuda._sleep(20_000_000)
+            if writer == "gather":
+                cache.gather_sequences(src, index)
+            else:
+                for l in (0, 1):
+                    cache.append_kv(l, more[0][l], more[1][l])
+            if cache is dst:
+                graphs.append(torch.cuda.CUDAGraph())
+                with torch.cuda.stream(side):
+                    graphs[-1].capture_begin()
+                    cache.decode_attention(layer, q, out=out)
+                    graphs[-1].capture_end()
+            result = cache.decode_attention(layer, q)
+            if cache is want:
+                expected = result
+        assert torch.equal(result, expected)
+    dst.check_device()
