@@ -227,7 +227,8 @@ int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, in
  * those), the softmax numerators rounded to half precision where io_dtype is bfloat16 (at
  * most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits where it is half precision; sums
  * are fp32.  Up to eight rows of a kv head: as xq_decode_attention.
- * XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.
+ * XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.  XQ_KERNEL_MMA: any shape over the prefix; own tokens of a
+ * shape that it does not take in a decode call (head_dim 64, more than eight heads) are XQ_ERR_CONFIG.
  * The _f32 variant writes float results (tests).  Errors as xq_attention_chunk; XQ_ERR_ARG also: both layers
  * empty, 0 < S < n_q_tokens, current device not the handles'; XQ_ERR_CAPACITY: workspace too small. */
 size_t xq_prefix_workspace_bytes(const xq_cache* c, const xq_cache* prefix, int n_q_tokens);
@@ -240,7 +241,7 @@ int xq_prefix_attention_f32(xq_cache* c, xq_cache* prefix, int layer, const void
  * against all tokens of `layer` (an encoder's states, say), none masked.  lengths: device, int32 [batch], or
  * NULL; sequence b has only its first lengths[b] tokens (values outside 0 .. S count as the nearer end), and
  * what the cache holds behind them reaches no result.  Length 0 gives zeros.  q, out, workspace, precision as
- * xq_prefix_attention.  Errors: XQ_ERR_ARG (also: empty layer), XQ_ERR_ORDER, XQ_ERR_CAPACITY, XQ_ERR_CUDA. */
+ * xq_prefix_attention; XQ_KERNEL_MMA: any shape.  Errors: XQ_ERR_ARG (also: empty layer), XQ_ERR_ORDER, XQ_ERR_CAPACITY, XQ_ERR_CUDA. */
 size_t xq_cross_workspace_bytes(const xq_cache* c, int n_q_tokens);
 int xq_cross_attention(xq_cache* c, int layer, const void* q, void* out, int n_q_tokens, const int32_t* lengths,
                        void* workspace, size_t workspace_bytes, void* stream);

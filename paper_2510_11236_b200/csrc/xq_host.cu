@@ -455,16 +455,8 @@ struct Scratch {
   int* status;
 };
 
-// Checks a decode call; nq packed and r window tokens are visible to it.  Touches no state.
-// K_new / V_new: one new token per stream that the tensor-core kernel appends itself; S is the layer's length with that
-// token counted.  vis >= 0: only the first vis tokens are visible to the query (a query token of a chunk that is
-// followed by later tokens in the cache).
-int check_decode(const xq_cache* c, int layer, const void* q, const void* out, const void* K_new, const void* V_new, int S,
-                 int vis, int& nq, int& r, bool& use_mma) {
-  if (!c || !q || !out) return XQ_ERR_ARG;
-  if (layer < 0 || layer >= c->cfg.n_layers) return XQ_ERR_ARG;
-  if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return XQ_ERR_ARG;
-  if (((uintptr_t)K_new & 15) || ((uintptr_t)V_new & 15)) return XQ_ERR_ARG;
+// The tokens of a layer that a call sees: nq packed and r window tokens of the layer's S (vis >= 0: of its first vis ones).
+int check_tokens(const xq_cache* c, int layer, int S, int vis, int& nq, int& r) {
   const Dims& dm = c->plan.dm;
   if (S < 1) return XQ_ERR_ARG;
   r = residual_count(S, dm.R);
@@ -477,6 +469,21 @@ int check_decode(const xq_cache* c, int layer, const void* q, const void* out, c
   for (int o : {k_owner(&c->cfg, layer), v_owner(&c->cfg, layer)}) {
     if (o != layer && c->seq[o] - residual_count(c->seq[o], dm.R) < nq) return XQ_ERR_ORDER;
   }
+  return XQ_OK;
+}
+
+// Checks a decode call; nq packed and r window tokens are visible to it.  Touches no state.
+// K_new / V_new: one new token per stream that the tensor-core kernel appends itself; S is the layer's length with that
+// token counted.  vis >= 0: only the first vis tokens are visible to the query (a query token of a chunk that is
+// followed by later tokens in the cache).
+int check_decode(const xq_cache* c, int layer, const void* q, const void* out, const void* K_new, const void* V_new, int S,
+                 int vis, int& nq, int& r, bool& use_mma) {
+  if (!c || !q || !out) return XQ_ERR_ARG;
+  if (layer < 0 || layer >= c->cfg.n_layers) return XQ_ERR_ARG;
+  if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return XQ_ERR_ARG;
+  if (((uintptr_t)K_new & 15) || ((uintptr_t)V_new & 15)) return XQ_ERR_ARG;
+  const int rc = check_tokens(c, layer, S, vis, nq, r);
+  if (rc != XQ_OK) return rc;
   use_mma = uses_mma(c);
   if (c->cfg.kernel >= XQ_KERNEL_MMA && !use_mma) return XQ_ERR_CONFIG;
   if (K_new && !use_mma) return XQ_ERR_ARG;
@@ -1315,7 +1322,7 @@ int prefix_impl(xq_cache* c, xq_cache* prefix, int layer, const void* q, void* o
   if (Sp == 0) return chunk_impl(c, layer, q, out, T, out_f32, stream);
   int nq, r;
   bool use_mma;
-  int rc = check_decode(prefix, layer, q, out, nullptr, nullptr, Sp, -1, nq, r, use_mma);
+  int rc = check_tokens(prefix, layer, Sp, -1, nq, r);
   if (rc == XQ_OK && S > 0) rc = check_decode(c, layer, q, out, nullptr, nullptr, S, S - T + 1, nq, r, use_mma);
   if (rc == XQ_OK && S > 0) rc = check_decode(c, layer, q, out, nullptr, nullptr, S, S, nq, r, use_mma);
   if (rc != XQ_OK) return rc;
@@ -1354,8 +1361,7 @@ int cross_impl(xq_cache* c, int layer, const void* q, void* out, int T, const in
   if (((uintptr_t)q & 15) || ((uintptr_t)out & 15) || ((uintptr_t)lengths & 3)) return XQ_ERR_ARG;
   const int S = c->seq[layer];
   int nq, r;
-  bool use_mma;
-  int rc = check_decode(c, layer, q, out, nullptr, nullptr, S, -1, nq, r, use_mma);
+  int rc = check_tokens(c, layer, S, -1, nq, r);
   if (rc != XQ_OK) return rc;
   const RowsPlan plan = rows_plan(c, c->cfg.batch, T);
   const int ns = rows_splits(c, plan, S);

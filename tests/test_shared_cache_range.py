@@ -192,3 +192,28 @@ def test_packed_elements_beyond_half_precision(shape, which, T, kernel):
             _compare(cfg, o32, o16, q, lambda b, h: [x[:n[b]] for x in _restored(cfg, K, V, layer, b, h)],
                      min(n[b], S - (S - 1) % R - 1), range(Hkv), [b], pairs, products=4, tokens=[0, T - 1])
     cache.check_device()
+
+
+# ---- the tensor-core kernel by name ----
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [SHAPES[5], SHAPES[3], SHAPES[4]])  # twelve heads on a kv head; head_dim 64
+def test_tensor_core_kernel_by_name(shape):
+    # the decode kernel of that name takes neither shape, the rows kernel any: over a whole cache there is nothing to refuse
+    named = dict(kernel=xq.XQ_KERNEL_MMA)
+    cp, cc = _shape(shape, batch=1, max_seq=300, **named), _shape(shape, batch=3, max_seq=200, **named)
+    kp, vp = _tokens(cp, 1, 300)
+    ko, vo = _tokens(cc, 2, 200)
+    prefix, cache, alone = _filled(cp, kp, vp), _filled(cc, ko, vo), xq.Cache(cc, DEV)
+    heads = range(cc.n_kv_heads)
+    for T in (1, 7):
+        q = _queries(cc, 3, T)
+        n = [S - (S - 1) % cc.residual_len - 1 for S in (300, 200)]
+        o32, o16 = (alone.prefix_attention(prefix, 1, q.to(DEV), f32=f32) for f32 in (True, False))
+        _compare(cc, o32, o16, q, lambda b, h: _restored(cp, kp, vp, 1, 0, h), n[0], heads, range(3), False)
+        o32, o16 = (cache.cross_attention(1, q.to(DEV), f32=f32) for f32 in (True, False))
+        _compare(cc, o32, o16, q, lambda b, h: _restored(cc, ko, vo, 1, b, h), n[1], heads, range(3), False)
+        with pytest.raises(xq.XQError) as e:  # the sequences' own tokens are the decode kernel's
+            cache.prefix_attention(prefix, 1, q.to(DEV))
+        assert e.value.code == xq.XQ_ERR_CONFIG
+    cache.check_device(), alone.check_device()
