@@ -8,7 +8,7 @@ import torch
 
 import paper_2510_11236_b200 as xq
 from tests import util
-from tests.test_shared_cache import DEV, KERNELS, SHAPES, _filled, _queries, _restored, _shape, _tokens
+from tests.test_shared_cache import DEV, KERNELS, SHAPES, _check, _filled, _queries, _restored, _shape, _tokens
 
 BLOCK = 128  # tokens whose window rows share an exponent
 
@@ -217,3 +217,159 @@ def test_tensor_core_kernel_by_name(shape):
             cache.prefix_attention(prefix, 1, q.to(DEV))
         assert e.value.code == xq.XQ_ERR_CONFIG
     cache.check_device(), alone.check_device()
+
+
+# ---- long caches: more splits than one trip of the join, than a warp of the decode kernels' merge ----
+
+def _splits_used(space, rows, D):
+    """Splits of a rows call, by how far it wrote its workspace (filled with 0xa5 before): partial sums, then two words a partial."""
+    end = int((space != 0xa5).nonzero().max()) + 1
+    for ns in range(1, 1000):
+        sums = -(-rows * ns * D * 4 // 256) * 256
+        if end <= sums + rows * ns * 8:
+            return ns if end > sums else 0
+    return 0
+
+
+LONG = [  # shape, tokens
+    ((128, 4, 1, 32, 128, 2, 0, False), 20011), ((128, 4, 1, 64, 256, 0, 2, True), 46000), ((64, 2, 1, 32, 64, 2, 2, False), 30000),
+    ((64, 8, 1, 64, 64, 0, 0, True), 23456),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("shape,S", LONG)
+def test_more_splits_than_one_trip_of_the_join(shape, S, kernel):
+    cfg = _shape(shape, batch=1, max_seq=S, kernel=kernel)
+    K, V = _tokens(cfg, 1, S)
+    cache = _filled(cfg, K, V)
+    T, n = 17, S - (S - 1) % cfg.residual_len - 1
+    q = _queries(cfg, 3, T)
+    space = torch.full((xq.xq_cross_workspace_bytes(cache.handle, T),), 0xa5, dtype=torch.uint8, device=DEV)
+    o32 = cache.cross_attention(1, q.to(DEV), f32=True, workspace=space)
+    assert _splits_used(space, T * cfg.n_q_heads, cfg.head_dim) > 16
+    o16 = cache.cross_attention(1, q.to(DEV))
+    _compare(cfg, o32, o16, q, lambda b, h: _restored(cfg, K, V, 1, b, h), n, [0], [0], False, tokens=[0, 16])
+    cache.check_device()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,S", LONG)
+def test_prefix_of_many_splits_behind_own_tokens(shape, S):
+    D, Hq, Hkv, g, R, kq, vq, f16 = shape
+    cp, cc = _shape(shape, batch=1, max_seq=S), _shape(shape, batch=17, max_seq=200)
+    kp, vp = _tokens(cp, 1, S)
+    ko, vo = _tokens(cc, 2, 70)
+    prefix, cache = _filled(cp, kp, vp), _filled(cc, ko, vo)
+    q = _queries(cc, 3, 1)
+    o32, o16 = (cache.prefix_attention(prefix, 1, q.to(DEV), f32=f32) for f32 in (True, False))
+    whole = _restored(cp, kp, vp, 1, 0, 0)
+    _check(cc, o32, o16, q, lambda b, h: whole, lambda b, h: _restored(cc, ko, vo, 1, b, h), 1, 70, batch=[0, 16], rows=17 * Hq)
+    cache.check_device()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,S", LONG)
+def test_more_splits_than_a_warp_of_the_merge(shape, S):
+    # up to eight rows of a kv head: the decode kernels, whose last CTA of a stream merges
+    cfg = _shape(shape, batch=1, max_seq=S)
+    K, V = _tokens(cfg, 1, S)
+    cache = _filled(cfg, K, V)
+    rc, splits, _ = xq.xq_split_plan(cache.handle, 1)
+    assert rc == 0 and splits > 32
+    n = S - (S - 1) % cfg.residual_len - 1
+    whole = _restored(cfg, K, V, 1, 0, 0)
+    for lengths in (None, [S - 5000], [1000]):
+        q = _queries(cfg, 3, 1)
+        ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+        o32, o16 = (cache.cross_attention(1, q.to(DEV), lengths=ln, f32=f32) for f32 in (True, False))
+        seen = S if lengths is None else lengths[0]
+        _compare(cfg, o32, o16, q, lambda b, h: [x[:seen] for x in whole], min(n, seen), [0], [0], False)
+    cache.check_device()
+
+
+# ---- logits that rise or fall through the tokens ----
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("T", [1, 17, 1300])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[1], SHAPES[3], SHAPES[6]])
+@pytest.mark.parametrize("course", ["rising", "falling", "waves", "equal"])
+def test_course_of_the_logits(course, shape, T, kernel):
+    # the reference of the softmax is raised in every tile, in none behind the first, in every other one
+    S = 1200
+    cfg = _shape(shape, batch=2, max_seq=S, kernel=kernel)
+    K, V = _tokens(cfg, 1, S, outliers=False)
+    t = torch.arange(S)
+    level = {"rising": t / S, "falling": 1 - t / S, "waves": ((t // 64) % 2) * (t / S), "equal": 0.0 * t}[course] * 200.0
+    rng = np.random.default_rng(7)
+    u = torch.from_numpy(rng.choice([-1.0, 1.0], cfg.head_dim)).float()
+    scale = 1 / math.sqrt(cfg.head_dim)
+    along = level[:, None] * u / (scale * cfg.head_dim)
+    K = [((0.0 if course == "equal" else 0.02) * x.float() + along).to(x.dtype) for x in K]
+    cache = _filled(cfg, K, V)
+    q = (_queries(cfg, 3, T).float() * 0.1 + u).to(K[0].dtype)
+    q[..., 1::2, :] *= -1  # every other head: the other way round
+    o32, o16 = (cache.cross_attention(1, q.to(DEV), f32=f32) for f32 in (True, False))
+    n = S - (S - 1) % cfg.residual_len - 1
+    _compare(cfg, o32, o16, q, lambda b, h: _restored(cfg, K, V, 1, b, h), n, [0, 1][:cfg.n_kv_heads], [0, 1],
+             cfg.io_dtype == xq.XQ_F16 and T * cfg.n_q_heads // cfg.n_kv_heads > 128, tokens=[0, T - 1])
+    cache.check_device()
+
+
+# ---- sharing patterns ----
+
+PATTERNS = [dict(n_layers=3, share_group=3, share_dominant=1), dict(n_layers=3, share_group=3, share_dominant=2),
+            dict(n_layers=4, share_group=4, share_dominant=0), dict(n_layers=4, share_group=4, share_dominant=3),
+            dict(n_layers=2, gamma1=0.4), dict(n_layers=2, share_dominant=1)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [2, 1])
+@pytest.mark.parametrize("pattern", PATTERNS)
+@pytest.mark.parametrize("D", [128, 64])
+def test_sharing_patterns(D, pattern, bits):
+    """Prefix, cross attention and gathered sequences over layers that share codes in other ways than pairs."""
+    L, S = pattern["n_layers"], 333
+    order = sorted(range(L), key=lambda l: l != pattern.get("share_dominant", 0))  # the layer that owns the codes first
+    kw = dict(head_dim=D, n_q_heads=6, n_kv_heads=2, group_size=32, residual_len=64, kq=L * (bits - 1), vq=L * (bits - 1), km=0, vm=0,
+              eta1=1 / 6, eta2=0.045, **pattern)
+    one, three = xq.make_config(batch=2, max_seq=S, **kw), xq.make_config(batch=6, max_seq=S, **kw)
+
+    def filled(cfg, K, V):
+        cache = xq.Cache(cfg, DEV)
+        for layer in order:
+            cache.append_kv(layer, K[layer].to(DEV), V[layer].to(DEV))
+        return cache
+
+    def tokens(cfg, seed, n):
+        K, V = _tokens(cfg, seed, n)
+        g = torch.Generator().manual_seed(seed + 50)
+        return [[(x[0].float() + 0.1 * torch.randn(x[0].shape, generator=g)).to(x[0].dtype) for _ in range(L)] for x in (K, V)]
+
+    def restored(cfg, K, V, layer, b, h):
+        oc = util.oracle_for_stream(cfg, order, b, h, {l: (K[l], V[l]) for l in order})
+        n, st, g = oc.n_quantized(layer), oc.layers[layer], cfg.group_size
+        kc, ks, kz, vc, vs, vz = (np.asarray(x[0, 0], dtype=np.float64) for x in oc.codes_and_meta(layer))
+        ks, kz, vs, vz = np.repeat(ks, g, 0), np.repeat(kz, g, 0), np.repeat(vs, g, 1), np.repeat(vz, g, 1)
+        k, v = (np.concatenate([x, st[w][0, 0]]) for x, w in ((kc * ks + kz, "win_k"), (vc * vs + vz, "win_v")))
+        ka, va = np.abs(k), np.abs(v)
+        ka[:n], va[:n] = (np.abs(kc - 1) + 1) * ks + np.abs(kz), (np.abs(vc - 1) + 1) * vs + np.abs(vz)
+        return k, v, ka, va
+
+    kp, vp = tokens(one, 1, S)
+    ko, vo = tokens(three, 2, 150)
+    prefix, cache, spare = filled(one, kp, vp), filled(three, ko, vo), xq.Cache(three, DEV)
+    index = torch.tensor([5, 0, 0, 3, 2, 1], dtype=torch.int32, device=DEV)
+    spare.gather_sequences(cache, index)
+    for layer in range(L):
+        for T in (1, 12):
+            q = _queries(three, 3 + layer, T)
+            o32, o16 = (cache.prefix_attention(prefix, layer, q.to(DEV), f32=f32) for f32 in (True, False))
+            _check(three, o32, o16, q, lambda b, h: restored(one, kp, vp, layer, b // 3, h), lambda b, h: restored(three, ko, vo, layer, b, h),
+                   T, 150, heads=[1], batch=[0, 5], rows=T * 9)
+            o32, o16 = (cache.cross_attention(layer, q.to(DEV), f32=f32) for f32 in (True, False))
+            _compare(three, o32, o16, q, lambda b, h: restored(three, ko, vo, layer, b, h), 128, [0], [0, 5], False)
+            assert torch.equal(spare.cross_attention(layer, q[:, index.long().cpu()].contiguous().to(DEV), f32=True), o32[:, index.long()])
+    cache.check_device(), spare.check_device()
