@@ -189,3 +189,40 @@ def test_a_captured_decode_says_nothing_about_calls_outside(writer):
                 expected = result
         assert torch.equal(result, expected)
     dst.check_device()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("each,T", [(1, 1), (2, 1), (12, 1), (3, 30)])  # decode, rows and chunk kernels
+def test_caches_that_use_one_prefix_at_once(each, T):
+    # two handles on two streams, eager and in two graphs: a prefix is only read, each handle has its own scratch and workspace
+    P, Sp = 3, 900
+    prefix = _filled(_config(batch=P, max_seq=Sp), *_tokens(_config(batch=P, max_seq=Sp), 1, Sp))
+    cfg = _config(batch=P * each, max_seq=400)
+    caches = [_filled(cfg, *_tokens(cfg, 2 + k, 250)) for k in range(2)]
+    qs = [_queries(cfg, 5 + k, T).to(DEV) for k in range(2)]
+    spaces = [torch.empty(xq.xq_prefix_workspace_bytes(c.handle, prefix.handle, T), dtype=torch.uint8, device=DEV) for c in caches]
+    want = [[c.prefix_attention(prefix, layer, q, f32=True) for layer in (0, 1)] for c, q in zip(caches, qs)]
+    outs = [[torch.empty_like(x) for x in w] for w in want]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in caches]
+
+    def calls(k):
+        for layer in (0, 1):
+            caches[k].prefix_attention(prefix, layer, qs[k], out=outs[k][layer], f32=True, workspace=spaces[k])
+    graphs = []
+    for k in (0, 1):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[k]):
+            calls(k)
+    for run in (calls, lambda k: graphs[k].replay()):
+        for x in outs[0] + outs[1]:
+            x.zero_()
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for k in (0, 1):
+                with torch.cuda.stream(streams[k]):
+                    run(k)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in (0, 1) for a, b in zip(outs[k], want[k]))
+    for c in caches:
+        c.check_device()
