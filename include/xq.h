@@ -225,8 +225,11 @@ int xq_attention_chunk_f32(xq_cache* c, int layer, const void* q, float* out, in
  * precision), window tokens as half precision relative to the
  * largest element of their 128 (values below 2^-46 of larger ones before them, packed ones counted as 1: to 2^-85 of
  * those), the softmax numerators rounded to half precision where io_dtype is bfloat16 (at
- * most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits where it is half precision; sums
- * are fp32.  Up to eight rows of a kv head: as xq_decode_attention.
+ * most 2^-11 of each; their sum is that of the rounded ones), as pairs of 22 bits where it is half precision, in both
+ * to no less than 2^-31 of the row's largest one; sums are fp32.  Up to eight rows of a kv head in a token, and up to 16
+ * tokens, may go to the decode kernels, token by token, where those are modelled to be faster: precision is then
+ * xq_decode_attention's.  Logits (scale included) below 2^24 in magnitude, in all of the tensor-core kernels: beyond, a
+ * row may come out as not a number.
  * XQ_KERNEL_GENERIC in c's configuration: fp32 throughout.  XQ_KERNEL_MMA: any shape over the prefix; own tokens of a
  * shape that it does not take in a decode call (head_dim 64, more than eight heads) are XQ_ERR_CONFIG.
  * The _f32 variant writes float results (tests).  Errors as xq_attention_chunk; XQ_ERR_ARG also: both layers

@@ -85,8 +85,9 @@ __device__ __forceinline__ Place place_of(const Launch& p, uint32_t item) {
   return r;
 }
 
-// From one cache to another: a thread holds its vectors of a source while the sequences that follow have the same one (a
-// prompt that is forked is read once).
+// From one cache to another: a thread holds its vectors of a source while the sequences that follow have the same one.  A prompt
+// that is forked into neighbouring sequences is read once by each item (of `parts` that share a piece's sequences); indices in
+// turn, 0, 1, 0, 1, fetch it each time, from L2 where it still is there.
 __global__ void __launch_bounds__(COPY_THREADS) gather_kernel(const __grid_constant__ Launch p) {
   const Place r = place_of<0>(p, blockIdx.x);
   int b0, b1;

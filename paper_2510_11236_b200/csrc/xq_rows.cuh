@@ -32,8 +32,9 @@
 // bfloat16 ones scaled by a power of two for each batch.
 //
 // Bound: not one pipe, but two chains of latencies that compete for issue slots (60 to 70 % of them, tensor pipe 41 %).  A batch of
-// 128 tokens takes 1.24 to 1.30 us a CTA, 2400 cycles (head_dim 128, bfloat16; half precision 1.50), whether 9 or 128 rows exist,
-// and a launch 9 us more.  Cycles of a batch: the products 1152 (half precision 1728).  S from its issue to the softmax warps 870,
+// 128 tokens takes 1.23 to 1.33 us a CTA, 2400 cycles (head_dim 128, bfloat16; half precision 1.51 to 1.59; head_dim 64 1.05 to
+// 1.13 and 1.26 to 1.36), whether 17 or 128 rows exist, and a launch 8 to 9 us more (half precision, head_dim 64: 5 to 7).  Cycles
+// of a batch: the products 1152 (half precision 1728).  S from its issue to the softmax warps 870,
 // the search 900, the turn 500, the numerators 1700, to the issuing warp 250, and two batches are in flight.  The expansion of a
 // batch's keys 2000 and 600 until the next one, values the same.  In copies: half of the expansion left out 0.57 us a tile for
 // 0.63.  Measured and not kept, us a tile against 0.62: three expanding groups of four warps that take keys and values in turn 0.64;
